@@ -63,11 +63,12 @@ typedef enum {
   SSTE_BF16 = 0,   /* bfloat16 */
   SSTE_F8E4M3 = 1, /* OCP FP8 e4m3fn: bias 7, max 448, no infinity */
   SSTE_F32 = 2,    /* float32: accepted only where an argument's description says so */
-  SSTE_F8E5M2 = 3  /* OCP FP8 e5m2 output gradients (the backward format of Sec. 5.2), accepted as `dtype` by
+  SSTE_F8E5M2 = 3, /* OCP FP8 e5m2 output gradients (the backward format of Sec. 5.2), accepted as `dtype` by
                       sste_linear_wgrad, sste_linear_dgrad and sste_mvue_materialize only: dY (and the
                       sparsified operand made from it) is e5m2, bias 15, max 57344, inputs finite; the
                       other operand of the call (X, or the packed weight) is SSTE_F8E4M3.  Sizes and
                       alignment follow SSTE_F8E4M3. */
+  SSTE_F8BLOCK = 4 /* e4m3 codes with a power of two for every 32 features (sste_checkpoint_pack): X of sste_adapter_wgrad only */
 } sste_dtype;
 
 /*
@@ -503,6 +504,80 @@ int sste_cast_fp8(const void* X, int64_t R, int64_t C, int64_t ldx, int out_dtyp
                   void* Q, int64_t ldq, float* amax_out, void* hip_stream);
 
 /*
+ * Low-rank adapters beside a shared projection (fine-tuning or serving many fine-tunes of one 2:4 model: the packed weight is shared and
+ * frozen, and every row of the batch adds the product of two thin matrices of its own adapter).  For a row of adapter n:
+ *
+ *   sste_adapter_fwd     S  = scale_n * x_scale * X A_n^T       Z  = RNE_bf16(base + S B_n)      base: Z of sste_linear_fwd
+ *   sste_adapter_dgrad   dS = scale_n * dz_scale * dZ B_n^T     dX = RNE_bf16(base + dS A_n)     base: dX of sste_linear_dgrad
+ *   sste_adapter_wgrad   dA_n (+)= x_scale * sum dS^T X         dB_n (+)= dz_scale * sum S^T dZ  sums over the rows of adapter n
+ *
+ * S and dS (T x R, float32) are outputs of the first two calls that the third takes; both contain scale_n, which is why dA and dB need it
+ * no more.  Products are accumulated in float32; S enters S B_n as the sum of two bf16, to within 2^-17 of
+ * itself (dS likewise), and the sums over rows as the sum of three, with all its bits.
+ *
+ *   row_start    in  device, int32, segments + 1 entries that do not decrease: segment s holds the rows row_start[s] .. row_start[s+1] - 1
+ *                    (a request, a sequence, a single token; empty ones are allowed)
+ *   seg_adapter  in  device, int32, its adapter; several segments may have the same one; anything outside 0 .. adapters - 1: none.
+ *                    Both arrays are read by the kernels: grids depend on T and `segments` alone, so a captured graph serves other bounds
+ *                    and other adapters.  They are clamped to the matrices: a malformed array gives unspecified results, never an access
+ *                    outside them.
+ *                    Rows of no adapter and rows of no segment (before the first, behind the last): S = 0, Z = base (0 if base is NULL; not
+ *                    written if Z is base), no part in dA and dB.
+ *   A, B         in  device, bf16, the adapters' matrices one below the other: A is adapters * R x I (leading dimension lda), B is
+ *                    adapters * R x O (ldb): B is kept with the rank along its rows, as A is.  Adapters of several ranks share a stack of the
+ *                    widest, the others' rows padded with zeros.
+ *   scale        in  device, float32, adapters entries, or NULL for 1
+ *   R            in  a multiple of 8 up to 128
+ *   dtype        in  of X: SSTE_BF16 (x_scale 1) or SSTE_F8E4M3; of dZ also SSTE_F8E5M2.  I and O: multiples of 8, of 16 where they are the width
+ *                    of an 8-bit operand; at most 2^24.  T < 2^30, segments <= 2^20, adapters <= 65535.
+ *   base         in  device, bf16, or NULL; may be Z (dX) itself, with the same leading dimension, and must not overlap it otherwise
+ *   S, dS        leading dimensions multiples of 4
+ */
+int sste_adapter_fwd(const void* X, int64_t T, int64_t I, int64_t ldx, int dtype, float x_scale,
+                     const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
+                     const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t O,
+                     const void* base, int64_t ldbase, void* Z, int64_t ldz, float* S, int64_t lds, void* hip_stream);
+int sste_adapter_dgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
+                       const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
+                       const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t I,
+                       const void* base, int64_t ldbase, void* dX, int64_t lddx, float* dS, int64_t ldds, void* hip_stream);
+/*
+ * The adapters' weight gradients.  X may also be a checkpoint (x_dtype SSTE_F8BLOCK: codes in X, scales in x_blocks with leading dimension ldxb,
+ * x_scale 1); otherwise x_blocks is ignored.  dA (adapters * R x I, ldda) and dB (adapters * R x O, lddb) are float32, leading dimensions multiples
+ * of 4; an adapter without rows gets zeros, or keeps what it has with accumulate = 1.  S and dS of rows without an adapter are not read.
+ * Each adapter's rows are summed in their order, in chunks that depend on T, I, O and the bounds: the same call gives the same bits.
+ * workspace: sste_adapter_wgrad_workspace_bytes(T, segments, R, I, O) bytes of device scratch, 16-byte aligned (0 on bad arguments).
+ */
+int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
+                       const void* X, int64_t I, int64_t ldx, int x_dtype, float x_scale, const void* x_blocks, int64_t ldxb,
+                       const float* S, int64_t lds, const float* dS, int64_t ldds,
+                       const int32_t* row_start, int64_t segments, const int32_t* seg_adapter, int64_t adapters, int64_t R,
+                       float* dA, int64_t ldda, float* dB, int64_t lddb, int accumulate,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t sste_adapter_wgrad_workspace_bytes(int64_t T, int64_t segments, int64_t R, int64_t I, int64_t O);
+
+/*
+ * Activation checkpoints in 8 bits: what the forward pass leaves for the backward pass (a layer's input, the pre-activations of the feed-forward
+ * block) in 1.03 bytes an element, and the backward pass's use of it.  Each row is cut into blocks of 32 features (the last may be shorter):
+ *
+ *   sste_checkpoint_pack      e = the least exponent >= -117 with max |x| <= 448 * 2^e over the block's finite elements,
+ *                             code = RNE_e4m3(x * 2^-e), scale byte = e + 127.  No element saturates; relative to an element the error is at
+ *                             most 2^-4, and below 2^-6 * 2^e an absolute 2^-10 * 2^e.  Infinities and NaN become NaN codes (0x7F or 0xFF) and
+ *                             leave the rest of their block alone.
+ *   sste_checkpoint_backward  h = code * 2^e (exact in bf16; a magnitude that pack rounded up to 2^128 comes back as an infinity);
+ *                             A = RNE_bf16(act(h)) if A is given: the checkpointed tensor itself (SSTE_ACT_NONE) or the activation that the
+ *                             next layer's weight gradient reads; dH = RNE_bf16(dA * act'(h)) if dA and dH are given (with SSTE_ACT_NONE: dA).
+ *                             act as in sste_linear_fwd_act.  dH may be dA itself, with the same leading dimension.
+ *
+ *   X, A, dA, dH   device, bf16, R x C, leading dimensions multiples of 8, 16-byte aligned; C a multiple of 16, at most 2^24; R < 2^31
+ *   codes          device, R x C bytes, ldc a multiple of 16, 16-byte aligned
+ *   scales         device, one byte a block, R x ceil(C / 32), leading dimension lds
+ */
+int sste_checkpoint_pack(const void* X, int64_t R, int64_t C, int64_t ldx, void* codes, int64_t ldc, void* scales, int64_t lds, void* hip_stream);
+int sste_checkpoint_backward(const void* codes, const void* scales, int64_t R, int64_t C, int64_t ldc, int64_t lds, int act,
+                             void* A, int64_t lda, const void* dA, int64_t ldda, void* dH, int64_t lddh, void* hip_stream);
+
+/*
  * Flip count of Sec. 3.3 (numerator of the flip rate r_k): number of positions whose recorded /
  * not-recorded state differs between two metadata arrays of the same O x I/8 shape.
  *   count_out  out  device uint64_t*; overwritten
@@ -527,7 +602,9 @@ typedef enum {
   SSTE_K_DGRAD = 5,          /* input-gradient dense GEMM */
   SSTE_K_SGD_PROJECT_PACK = 6, /* dense-weight update fused with projection + pack */
   SSTE_K_CAST = 7,           /* per-tensor rescale + cast to an 8-bit format */
-  SSTE_K_COUNT = 8
+  SSTE_K_ADAPTER = 8,        /* low-rank adapters: both products of a call, or the weight gradients and their sum */
+  SSTE_K_CHECKPOINT = 9,     /* activation checkpoints */
+  SSTE_K_COUNT = 10
 } sste_kernel_id;
 int sste_timing_begin(int max_launches);
 int sste_timing_end(double* total_ms, int* launches);

@@ -10,10 +10,17 @@ from .binding import (  # noqa: F401
     BF16,
     F8E4M3,
     F8E5M2,
+    F8BLOCK,
     F32,
     PackBatch,
     SsteError,
+    adapter_dgrad,
+    adapter_fwd,
+    adapter_wgrad,
+    adapter_wgrad_workspace_bytes,
     cast_fp8,
+    checkpoint_backward,
+    checkpoint_pack,
     UpdateBatch,
     compute_beta,
     describe_plan,

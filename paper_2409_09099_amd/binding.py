@@ -20,6 +20,7 @@ BF16 = 0
 F8E4M3 = 1
 F32 = 2
 F8E5M2 = 3         # e5m2 output gradients against e4m3 operands: backward calls only
+F8BLOCK = 4        # e4m3 codes with a power of two for every 32 features (checkpoint_pack): X of adapter_wgrad only
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libsste.so")
@@ -90,6 +91,19 @@ def library() -> ctypes.CDLL:
     lib.sste_beta_workspace_bytes.restype = sz
     lib.sste_cast_fp8.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, vp, vp]
     lib.sste_flip_count.argtypes = [vp, vp, i64, i64, vp, vp]
+    lib.sste_adapter_fwd.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.sste_adapter_fwd.restype = ci
+    lib.sste_adapter_dgrad.argtypes = lib.sste_adapter_fwd.argtypes
+    lib.sste_adapter_dgrad.restype = ci
+    lib.sste_adapter_wgrad.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, i64, ci, f32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64,
+                                       vp, i64, vp, i64, ci, vp, sz, vp]
+    lib.sste_adapter_wgrad.restype = ci
+    lib.sste_adapter_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.sste_adapter_wgrad_workspace_bytes.restype = sz
+    lib.sste_checkpoint_pack.argtypes = [vp, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.sste_checkpoint_pack.restype = ci
+    lib.sste_checkpoint_backward.argtypes = [vp, vp, i64, i64, i64, i64, ci, vp, i64, vp, i64, vp, i64, vp]
+    lib.sste_checkpoint_backward.restype = ci
     lib.sste_timing_begin.argtypes = [ci]
     lib.sste_timing_begin.restype = ci
     lib.sste_timing_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ci)]
@@ -133,7 +147,7 @@ def _matrix(t: torch.Tensor, itemsize: int, name: str) -> Tuple[int, int, int]:
 
 
 def _esize(dtype: int) -> int:
-    return 1 if dtype in (F8E4M3, F8E5M2) else 2
+    return 1 if dtype in (F8E4M3, F8E5M2, F8BLOCK) else 2
 
 
 def packed_buffers(R: int, K: int, dtype: int, device):
@@ -438,6 +452,163 @@ def cast_fp8(X: torch.Tensor, scale: float, out_dtype: int = F8E4M3, Q: Optional
     return (Q if store else None), amax_out
 
 
+def _stack(t: torch.Tensor, itemsize: int, name: str) -> Tuple[int, int, int, int]:
+    """(adapters, rank, width, leading dimension in elements) of a stack of matrices, one below the other."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be 3-D (adapters, rank, width)")
+    n, R, width = t.shape
+    ld = _matrix(t[0], itemsize, name)[2] if n else width
+    if n > 1 and t.stride(0) != R * ld:
+        raise ValueError(f"{name}: the adapters' matrices must lie one below the other")
+    return n, R, width, ld
+
+
+def _segments(row_start: torch.Tensor, seg_adapter: torch.Tensor) -> int:
+    """Number of segments; the arrays as sste_adapter_fwd describes them."""
+    for t, name in ((row_start, "row_start"), (seg_adapter, "seg_adapter")):
+        if t.dim() != 1 or t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous 1-D int32 tensor on the GPU")
+    if row_start.shape[0] != seg_adapter.shape[0] + 1:
+        raise ValueError("row_start must have one entry more than seg_adapter")
+    return seg_adapter.shape[0]
+
+
+def _adapter_arguments(X, x_name, row_start, seg_adapter, A, B, scale, dtype):
+    """What adapter_fwd and adapter_dgrad check alike: (T, width, ldx, segments, adapters, rank, I, lda, O, ldb)."""
+    T, width, ldx = _matrix(X, _esize(dtype), x_name)
+    segments = _segments(row_start, seg_adapter)
+    n, R, I, lda = _stack(A, 2, "A")
+    n2, R2, O, ldb = _stack(B, 2, "B")
+    if (n, R) != (n2, R2):
+        raise ValueError("A and B must have the same number of adapters and the same rank")
+    if scale is not None and (tuple(scale.shape) != (n,) or scale.dtype != torch.float32 or not scale.is_cuda or not scale.is_contiguous()):
+        raise ValueError("scale must be a contiguous float32 tensor on the GPU with one entry for each adapter")
+    return T, width, ldx, segments, n, R, I, lda, O, ldb
+
+
+def _result(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, like: torch.Tensor, name: str):
+    """The caller's rows x cols output, or a new one, and its leading dimension."""
+    if t is None:
+        t = torch.empty((rows, cols), dtype=dtype, device=like.device)
+    r, c, ld = _matrix(t, t.element_size(), name)
+    if (r, c) != (rows, cols) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {rows} x {cols} tensor of {dtype}")
+    return t, ld
+
+
+def _given(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, name: str) -> int:
+    """Leading dimension of an input of a known shape; 0 if there is none."""
+    if t is None:
+        return 0
+    r, c, ld = _matrix(t, t.element_size(), name)
+    if (r, c) != (rows, cols) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {rows} x {cols} tensor of {dtype}")
+    return ld
+
+
+def adapter_fwd(X: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, dtype: int = BF16, x_scale: float = 1.0,
+                Z: Optional[torch.Tensor] = None, S: Optional[torch.Tensor] = None):
+    """sste_adapter_fwd: S = scale_n x_scale X A_n^T (float32) and Z = base + S B_n (bf16), n the adapter of each row.  A is (adapters, rank, I)
+    and B (adapters, rank, O), bf16; rows row_start[s] .. row_start[s + 1] - 1 use adapter seg_adapter[s], or none (-1).  Z may be base.
+    Returns (Z, S)."""
+    T, I, ldx, segments, n, R, Ia, lda, O, ldb = _adapter_arguments(X, "X", row_start, seg_adapter, A, B, scale, dtype)
+    if Ia != I:
+        raise ValueError("A must be as wide as X")
+    Z, ldz = _result(Z, T, O, torch.bfloat16, X, "Z")
+    S, lds = _result(S, T, R, torch.float32, X, "S")
+    ldbase = _given(base, T, O, torch.bfloat16, "base")
+    _check(library().sste_adapter_fwd(_ptr(X), T, I, ldx, dtype, x_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
+                                      _ptr(scale), n, R, O, _ptr(base), ldbase, _ptr(Z), ldz, _ptr(S), lds, _stream(X)))
+    return Z, S
+
+
+def adapter_dgrad(dZ: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                  scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, dtype: int = BF16, dy_scale: float = 1.0,
+                  dX: Optional[torch.Tensor] = None, dS: Optional[torch.Tensor] = None):
+    """sste_adapter_dgrad: dS = scale_n dy_scale dZ B_n^T (float32) and dX = base + dS A_n (bf16); the rest as adapter_fwd.  Returns (dX, dS)."""
+    T, O, lddz, segments, n, R, I, lda, Ob, ldb = _adapter_arguments(dZ, "dZ", row_start, seg_adapter, A, B, scale, dtype)
+    if Ob != O:
+        raise ValueError("B must be as wide as dZ")
+    dX, lddx = _result(dX, T, I, torch.bfloat16, dZ, "dX")
+    dS, ldds = _result(dS, T, R, torch.float32, dZ, "dS")
+    ldbase = _given(base, T, I, torch.bfloat16, "base")
+    _check(library().sste_adapter_dgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
+                                        _ptr(scale), n, R, I, _ptr(base), ldbase, _ptr(dX), lddx, _ptr(dS), ldds, _stream(dZ)))
+    return dX, dS
+
+
+def adapter_wgrad_workspace_bytes(T: int, segments: int, R: int, I: int, O: int) -> int:
+    return int(library().sste_adapter_wgrad_workspace_bytes(T, segments, R, I, O))
+
+
+def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor,
+                  adapters: int, dtype: int = BF16, dy_scale: float = 1.0, x_dtype: int = BF16, x_scale: float = 1.0,
+                  x_blocks: Optional[torch.Tensor] = None, dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
+                  accumulate: bool = False, workspace: Optional[torch.Tensor] = None):
+    """sste_adapter_wgrad: dA_n (+)= x_scale sum dS^T X and dB_n (+)= dy_scale sum S^T dZ over the rows of each adapter, float32.  x_dtype F8BLOCK:
+    X holds the codes and x_blocks the scales of a checkpoint (checkpoint_pack).  Returns (dA (adapters, rank, I), dB (adapters, rank, O))."""
+    T, O, lddz = _matrix(dZ, _esize(dtype), "dZ")
+    T2, I, ldx = _matrix(X, _esize(x_dtype), "X")
+    if T2 != T:
+        raise ValueError("dZ and X must have the same number of rows (tokens)")
+    segments = _segments(row_start, seg_adapter)
+    if S.dim() != 2:
+        raise ValueError("S must be 2-D")
+    R = S.shape[1]
+    lds, ldds = _given(S, T, R, torch.float32, "S"), _given(dS, T, R, torch.float32, "dS")
+    ldxb = 0
+    if x_dtype == F8BLOCK:
+        if x_blocks is None:
+            raise ValueError("a checkpoint of X needs its scales (x_blocks)")
+        ldxb = _given(x_blocks, T, (I + 31) // 32, torch.uint8, "x_blocks")
+    if accumulate and (dA is None or dB is None):
+        raise ValueError("accumulate needs existing dA and dB")
+    dA = torch.empty((adapters, R, I), dtype=torch.float32, device=X.device) if dA is None else dA
+    dB = torch.empty((adapters, R, O), dtype=torch.float32, device=X.device) if dB is None else dB
+    na, Ra, Ia, ldda = _stack(dA, 4, "dA")
+    nb, Rb, Ob, lddb = _stack(dB, 4, "dB")
+    if (na, Ra, Ia, nb, Rb, Ob) != (adapters, R, I, adapters, R, O) or dA.dtype != torch.float32 or dB.dtype != torch.float32:
+        raise ValueError("dA and dB must be float32 tensors (adapters, rank, I) and (adapters, rank, O)")
+    if workspace is None:
+        workspace = torch.empty(adapter_wgrad_workspace_bytes(T, segments, R, I, O), dtype=torch.uint8, device=X.device)
+    _check(library().sste_adapter_wgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(X), I, ldx, x_dtype, x_scale, _ptr(x_blocks), ldxb, _ptr(S), lds,
+                                        _ptr(dS), ldds, _ptr(row_start), segments, _ptr(seg_adapter), adapters, R, _ptr(dA), ldda, _ptr(dB), lddb,
+                                        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(X)))
+    return dA, dB
+
+
+def checkpoint_pack(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
+    """sste_checkpoint_pack: X (bf16) as e4m3 codes with a power of two for every 32 features of a row.  Returns (codes (R, C) uint8,
+    scales (R, ceil(C / 32)) uint8)."""
+    R, C, ldx = _matrix(X, 2, "X")
+    codes, ldc = _result(codes, R, C, torch.uint8, X, "codes")
+    scales, lds = _result(scales, R, (C + 31) // 32, torch.uint8, X, "scales")
+    _check(library().sste_checkpoint_pack(_ptr(X), R, C, ldx, _ptr(codes), ldc, _ptr(scales), lds, _stream(X)))
+    return codes, scales
+
+
+def checkpoint_backward(codes: torch.Tensor, scales: torch.Tensor, dA: Optional[torch.Tensor] = None, act: int = ACT_GELU_TANH,
+                        A: Optional[torch.Tensor] = None, dH: Optional[torch.Tensor] = None, restore: bool = True):
+    """sste_checkpoint_backward: of the checkpointed H, A = act(H) (if restore) and dH = dA * act'(H) (if dA is given), both bf16.  With ACT_NONE, A is
+    the checkpointed tensor itself.  dH may be dA.  Returns (A or None, dH or None)."""
+    R, C, ldc = _matrix(codes, 1, "codes")
+    lds = _given(scales, R, (C + 31) // 32, torch.uint8, "scales")
+    lda = lddh = 0
+    if restore:
+        A, lda = _result(A, R, C, torch.bfloat16, codes, "A")
+    elif A is not None:
+        raise ValueError("A is given, but restore is False")
+    ldda = _given(dA, R, C, torch.bfloat16, "dA")
+    if dA is not None:
+        dH, lddh = _result(dH, R, C, torch.bfloat16, codes, "dH")
+    elif dH is not None:
+        raise ValueError("dH needs dA")
+    _check(library().sste_checkpoint_backward(_ptr(codes), _ptr(scales), R, C, ldc, lds, act, _ptr(A), lda, _ptr(dA), ldda, _ptr(dH), lddh,
+                                              _stream(codes)))
+    return A, dH
+
+
 def mvue_materialize(dY: torch.Tensor, seed: int, offset: int, dtype: int = BF16, first_token: int = 0):
     """sste_mvue_materialize(_at): MVUE(dY^T) as a packed 2:4 operand.  Returns (vals (O, T/2), meta (O, T/8))."""
     T, O, lddy = _matrix(dY, _esize(dtype), "dY")
@@ -482,7 +653,7 @@ def describe_plan(op: str, T: int, O: int, I: int, dtype: int = BF16) -> str:
     return text.value.decode()
 
 
-KERNEL_NAMES = ("project_pack", "fwd", "wgrad", "wgrad_reduce", "mvue_pack", "dgrad", "sgd_project_pack", "cast")
+KERNEL_NAMES = ("project_pack", "fwd", "wgrad", "wgrad_reduce", "mvue_pack", "dgrad", "sgd_project_pack", "cast", "adapter", "checkpoint")
 
 
 def timing_begin(max_launches: int = 4096) -> None:

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsste.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 
-SOURCES = ["api.hip", "prune_pack.hip", "gemm_fwd.hip", "gemm_wgrad.hip", "gemm_wgrad_fused.hip", "gemm_dgrad.hip", "cast.hip"]
+SOURCES = ["api.hip", "prune_pack.hip", "gemm_fwd.hip", "gemm_wgrad.hip", "gemm_wgrad_fused.hip", "gemm_dgrad.hip", "cast.hip",
+           "adapter_api.hip", "adapter.hip", "checkpoint.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",
