@@ -529,18 +529,22 @@ int sste_cast_fp8(const void* X, int64_t R, int64_t C, int64_t ldx, int out_dtyp
  *   scale        in  device, float32, adapters entries, or NULL for 1
  *   R            in  a multiple of 8 up to 128
  *   dtype        in  of X: SSTE_BF16 (x_scale 1) or SSTE_F8E4M3; of dZ also SSTE_F8E5M2.  I and O: multiples of 8, of 16 where they are the width
- *                    of an 8-bit operand; at most 2^24.  T < 2^30, segments <= 2^20, adapters <= 65535.
+ *                    of an 8-bit operand; they and all leading dimensions at most 2^23.  T < 2^30, segments <= 2^20, adapters <= 65535.
  *   base         in  device, bf16, or NULL; may be Z (dX) itself, with the same leading dimension, and must not overlap it otherwise
  *   S, dS        leading dimensions multiples of 4
+ *   workspace    device scratch of sste_adapter_workspace_bytes(T, segments, R, in, out) bytes, 16-byte aligned, with in and out the widths of X and Z
+ *                (of dZ and dX): few rows share the first product's contraction out among workgroups, whose sums are added in a fixed order.  With
+ *                less, or NULL, it is not shared out: slower, and the sums in another order.
  */
 int sste_adapter_fwd(const void* X, int64_t T, int64_t I, int64_t ldx, int dtype, float x_scale,
                      const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
                      const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t O,
-                     const void* base, int64_t ldbase, void* Z, int64_t ldz, float* S, int64_t lds, void* hip_stream);
+                     const void* base, int64_t ldbase, void* Z, int64_t ldz, float* S, int64_t lds, void* workspace, size_t workspace_bytes, void* hip_stream);
 int sste_adapter_dgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
                        const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
                        const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t I,
-                       const void* base, int64_t ldbase, void* dX, int64_t lddx, float* dS, int64_t ldds, void* hip_stream);
+                       const void* base, int64_t ldbase, void* dX, int64_t lddx, float* dS, int64_t ldds, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t sste_adapter_workspace_bytes(int64_t T, int64_t segments, int64_t R, int64_t in, int64_t out);
 /*
  * The adapters' weight gradients.  X may also be a checkpoint (x_dtype SSTE_F8BLOCK: codes in X, scales in x_blocks with leading dimension ldxb,
  * x_scale 1); otherwise x_blocks is ignored.  dA (adapters * R x I, ldda) and dB (adapters * R x O, lddb) are float32, leading dimensions multiples
@@ -569,7 +573,7 @@ size_t sste_adapter_wgrad_workspace_bytes(int64_t T, int64_t segments, int64_t R
  *                             next layer's weight gradient reads; dH = RNE_bf16(dA * act'(h)) if dA and dH are given (with SSTE_ACT_NONE: dA).
  *                             act as in sste_linear_fwd_act.  dH may be dA itself, with the same leading dimension.
  *
- *   X, A, dA, dH   device, bf16, R x C, leading dimensions multiples of 8, 16-byte aligned; C a multiple of 16, at most 2^24; R < 2^31
+ *   X, A, dA, dH   device, bf16, R x C, leading dimensions multiples of 8, 16-byte aligned; C a multiple of 16; C and these leading dimensions at most 2^23; R < 2^31
  *   codes          device, R x C bytes, ldc a multiple of 16, 16-byte aligned
  *   scales         device, one byte a block, R x ceil(C / 32), leading dimension lds
  */

@@ -18,6 +18,7 @@ from .binding import (  # noqa: F401
     adapter_fwd,
     adapter_wgrad,
     adapter_wgrad_workspace_bytes,
+    adapter_workspace_bytes,
     cast_fp8,
     checkpoint_backward,
     checkpoint_pack,

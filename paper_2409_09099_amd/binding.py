@@ -91,7 +91,9 @@ def library() -> ctypes.CDLL:
     lib.sste_beta_workspace_bytes.restype = sz
     lib.sste_cast_fp8.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, vp, vp]
     lib.sste_flip_count.argtypes = [vp, vp, i64, i64, vp, vp]
-    lib.sste_adapter_fwd.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.sste_adapter_fwd.argtypes = [vp, i64, i64, i64, ci, f32, vp, i64, vp, vp, i64, vp, i64, vp, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+    lib.sste_adapter_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.sste_adapter_workspace_bytes.restype = sz
     lib.sste_adapter_fwd.restype = ci
     lib.sste_adapter_dgrad.argtypes = lib.sste_adapter_fwd.argtypes
     lib.sste_adapter_dgrad.restype = ci
@@ -506,9 +508,22 @@ def _given(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, 
     return ld
 
 
+def _bytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def adapter_workspace_bytes(T: int, segments: int, R: int, width_in: int, width_out: int) -> int:
+    return int(library().sste_adapter_workspace_bytes(T, segments, R, width_in, width_out))
+
+
+def _adapter_workspace(given, T, segments, R, width_in, width_out, like):
+    need = adapter_workspace_bytes(T, segments, R, width_in, width_out) if given is None else 0
+    return torch.empty(need, dtype=torch.uint8, device=like.device) if need > 0 else given
+
+
 def adapter_fwd(X: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
                 scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, dtype: int = BF16, x_scale: float = 1.0,
-                Z: Optional[torch.Tensor] = None, S: Optional[torch.Tensor] = None):
+                Z: Optional[torch.Tensor] = None, S: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """sste_adapter_fwd: S = scale_n x_scale X A_n^T (float32) and Z = base + S B_n (bf16), n the adapter of each row.  A is (adapters, rank, I)
     and B (adapters, rank, O), bf16; rows row_start[s] .. row_start[s + 1] - 1 use adapter seg_adapter[s], or none (-1).  Z may be base.
     Returns (Z, S)."""
@@ -518,14 +533,15 @@ def adapter_fwd(X: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Ten
     Z, ldz = _result(Z, T, O, torch.bfloat16, X, "Z")
     S, lds = _result(S, T, R, torch.float32, X, "S")
     ldbase = _given(base, T, O, torch.bfloat16, "base")
+    workspace = _adapter_workspace(workspace, T, segments, R, I, O, X)
     _check(library().sste_adapter_fwd(_ptr(X), T, I, ldx, dtype, x_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
-                                      _ptr(scale), n, R, O, _ptr(base), ldbase, _ptr(Z), ldz, _ptr(S), lds, _stream(X)))
+                                      _ptr(scale), n, R, O, _ptr(base), ldbase, _ptr(Z), ldz, _ptr(S), lds, _ptr(workspace), _bytes(workspace), _stream(X)))
     return Z, S
 
 
 def adapter_dgrad(dZ: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
                   scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, dtype: int = BF16, dy_scale: float = 1.0,
-                  dX: Optional[torch.Tensor] = None, dS: Optional[torch.Tensor] = None):
+                  dX: Optional[torch.Tensor] = None, dS: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """sste_adapter_dgrad: dS = scale_n dy_scale dZ B_n^T (float32) and dX = base + dS A_n (bf16); the rest as adapter_fwd.  Returns (dX, dS)."""
     T, O, lddz, segments, n, R, I, lda, Ob, ldb = _adapter_arguments(dZ, "dZ", row_start, seg_adapter, A, B, scale, dtype)
     if Ob != O:
@@ -533,8 +549,10 @@ def adapter_dgrad(dZ: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.
     dX, lddx = _result(dX, T, I, torch.bfloat16, dZ, "dX")
     dS, ldds = _result(dS, T, R, torch.float32, dZ, "dS")
     ldbase = _given(base, T, I, torch.bfloat16, "base")
+    workspace = _adapter_workspace(workspace, T, segments, R, O, I, dZ)
     _check(library().sste_adapter_dgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
-                                        _ptr(scale), n, R, I, _ptr(base), ldbase, _ptr(dX), lddx, _ptr(dS), ldds, _stream(dZ)))
+                                        _ptr(scale), n, R, I, _ptr(base), ldbase, _ptr(dX), lddx, _ptr(dS), ldds, _ptr(workspace), _bytes(workspace),
+                                        _stream(dZ)))
     return dX, dS
 
 
@@ -574,7 +592,7 @@ def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.
         workspace = torch.empty(adapter_wgrad_workspace_bytes(T, segments, R, I, O), dtype=torch.uint8, device=X.device)
     _check(library().sste_adapter_wgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(X), I, ldx, x_dtype, x_scale, _ptr(x_blocks), ldxb, _ptr(S), lds,
                                         _ptr(dS), ldds, _ptr(row_start), segments, _ptr(seg_adapter), adapters, R, _ptr(dA), ldda, _ptr(dB), lddb,
-                                        int(bool(accumulate)), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(X)))
+                                        int(bool(accumulate)), _ptr(workspace), _bytes(workspace), _stream(X)))
     return dA, dB
 
 
@@ -671,10 +689,11 @@ def timing_end():
 
 # ---- native marshalling of the per-layer calls -------------------------------------------------------------
 _PYTHON = {f.__name__: f for f in (project_pack, sgd_project_pack, linear_fwd, linear_fwd_ex, linear_fwd_act, linear_dgrad, linear_dgrad_act,
-                                   linear_wgrad, cast_fp8)}
+                                   linear_wgrad, cast_fp8, adapter_fwd, adapter_dgrad, adapter_wgrad, checkpoint_pack, checkpoint_backward)}
 _NATIVE_ENTRY_POINTS = ("sste_project_pack_gamma", "sste_sgd_project_pack", "sste_linear_fwd_ex", "sste_linear_fwd_act", "sste_linear_dgrad_act",
                         "sste_linear_wgrad_at", "sste_wgrad_workspace_bytes", "sste_cast_fp8", "sste_project_pack_batch",
-                        "sste_sgd_project_pack_batch", "sste_last_error")
+                        "sste_sgd_project_pack_batch", "sste_adapter_fwd", "sste_adapter_dgrad", "sste_adapter_wgrad",
+                        "sste_adapter_workspace_bytes", "sste_adapter_wgrad_workspace_bytes", "sste_checkpoint_pack", "sste_checkpoint_backward", "sste_last_error")
 
 
 def _native_doc(f) -> str:

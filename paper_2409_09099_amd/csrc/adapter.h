@@ -4,18 +4,12 @@
 
 namespace sste {
 
-// 16 (8) bytes at p, zeros where `ok` is false.  (As a conditional expression of two lvalues the choice falls on the address, and the load becomes a flat one.)
+// 16 bytes at p, zeros where `ok` is false.  (As a conditional expression of two lvalues the choice falls on the address, and the load becomes a flat one.)
 __device__ __forceinline__ uint4 load16(const void* p, bool ok) {
   uint4 v = make_uint4(0, 0, 0, 0);
   if (ok) v = *(const uint4*)p;
   return v;
 }
-__device__ __forceinline__ uint2 load8(const void* p, bool ok) {
-  uint2 v = make_uint2(0, 0);
-  if (ok) v = *(const uint2*)p;
-  return v;
-}
-
 // Rows of a batch by segments, as the caller's device arrays give them: segment s holds the rows row_start[s] .. row_start[s + 1] - 1 and
 // uses adapter[s]; a number outside 0 .. adapters - 1 means none.
 struct AdapterSegments {
@@ -26,7 +20,7 @@ struct AdapterSegments {
 
 // Widest low rank, and its granule; most rows and segments (row numbers and tile numbers fit 32 bits)
 constexpr int kAdapterMaxRank = 128, kAdapterRankStep = 8;
-constexpr int64_t kAdapterMaxRows = 1ll << 30, kAdapterMaxSegments = 1ll << 20, kAdapterMaxAdapters = 65535, kAdapterMaxWidth = 1ll << 24;
+constexpr int64_t kAdapterMaxRows = 1ll << 30, kAdapterMaxSegments = 1ll << 20, kAdapterMaxAdapters = 65535, kAdapterMaxWidth = 1ll << 23;
 
 // D = scale_n x_scale X down_n^T (T x R float32), out = base + D up_n (T x C bf16).  X is T x K of dtype; down_n is R x K, up_n is R x C, stacked.
 struct AdapterApply {
@@ -47,7 +41,9 @@ struct AdapterApply {
   int64_t ldout;
   float* D;
   int64_t ldd;
+  float* ws;                // adapter_apply_workspace_bytes of it, or NULL
 };
+size_t adapter_apply_workspace_bytes(int64_t T, int segments, int R, int64_t K, int64_t C);
 hipError_t launch_adapter_apply(const AdapterApply& a, hipStream_t s);
 
 // One of the two weight gradients: G_n (R x C float32, stacked) (+)= m_scale sum over the rows of adapter n of L^T M, L T x R float32, M T x C.

@@ -35,11 +35,12 @@ __device__ __forceinline__ int segment_adapter(const AdapterSegments& g, int v) 
   const int n = g.adapter[v - 1];
   return n >= 0 && n < g.adapters ? n : -1;
 }
-// Every wave finds its tile by itself: 64 probes a round, so two rounds serve 4096 segments.
+// Every wave finds its tile by itself, 64 probes a round.  The last round (the only one up to 62 segments) has the adapters and the bounds that
+// follow among its probes, so that a workgroup waits for one load before it knows its rows.
 __device__ __forceinline__ Tile find_tile(const AdapterSegments& g, int slot, int tr) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = g.segments + 2;
-  while (n > 1) {
+  while (n > 63) {
     const int step = (n + 63) / 64;
     const int v = lo + lane * step;
     const bool before = lane * step < n && first_slot(g, v, tr) <= slot;
@@ -48,34 +49,39 @@ __device__ __forceinline__ Tile find_tile(const AdapterSegments& g, int slot, in
     n = min(step, n - hit * step);
     lo += hit * step;
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
+  const int v = lo + lane, bound = segment_bound(g, v), adapter = segment_adapter(g, v);
+  const uint64_t mask = __ballot(lane < n && (int)((uint32_t)bound / (uint32_t)tr) + v <= slot) | 1;
+  const int hit = __builtin_amdgcn_readfirstlane(63 - __clzll((long long)mask));       // at most 62: the next lane has the next bound
+  const int b0 = __builtin_amdgcn_readlane(bound, hit), b1 = __builtin_amdgcn_readlane(bound, hit + 1);
   Tile t;
-  t.row = segment_bound(g, lo) + (int64_t)(slot - first_slot(g, lo, tr)) * tr;
-  t.rows = (int)min((int64_t)tr, segment_bound(g, lo + 1) - t.row);
-  t.adapter = segment_adapter(g, lo);
+  t.row = b0 + (int64_t)(slot - (int)((uint32_t)b0 / (uint32_t)tr) - lo - hit) * tr;
+  t.rows = (int)min((int64_t)tr, b1 - t.row);
+  t.adapter = __builtin_amdgcn_readlane(adapter, hit);
   return t;
 }
 int64_t slots(const AdapterSegments& g, int tr) { return (int64_t)g.T / tr + g.segments + 2; }
 
 // ---- operands -------------------------------------------------------------------------------------------------
-// Eight consecutive elements as bf16.  8-bit formats convert exactly (e4m3 and e5m2 are subsets of bf16).
+// Consecutive elements as bf16, times a power of two.  8-bit formats convert exactly (e4m3 and e5m2 are subsets of bf16).
 enum { M_BF16 = 0, M_E4M3 = 1, M_E5M2 = 2, M_BLOCK = 3 };
+template <int DT>
+__device__ __forceinline__ void widen4(uint32_t& lo, uint32_t& hi, uint32_t c, float s) {
+  bf16x2 v[2];
+  if (DT == M_E5M2) {
+    v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, s, false);
+    v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, s, true);
+  } else {
+    v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false);
+    v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true);
+  }
+  __builtin_memcpy(&lo, &v[0], 4);
+  __builtin_memcpy(&hi, &v[1], 4);
+}
 template <int DT>
 __device__ __forceinline__ uint4 widen(uint2 c, float s) {
   uint4 r;
-  bf16x2 v[4];
-  if (DT == M_E5M2) {
-    v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c.x, s, false);
-    v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c.x, s, true);
-    v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c.y, s, false);
-    v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c.y, s, true);
-  } else {
-    v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, s, false);
-    v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, s, true);
-    v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, s, false);
-    v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, s, true);
-  }
-  __builtin_memcpy(&r, v, 16);
+  widen4<DT>(r.x, r.y, c.x, s);
+  widen4<DT>(r.z, r.w, c.y, s);
   return r;
 }
 __device__ __forceinline__ bf16x8 frag(uint4 v) {
@@ -83,19 +89,9 @@ __device__ __forceinline__ bf16x8 frag(uint4 v) {
   __builtin_memcpy(&r, &v, 16);
   return r;
 }
-// A float as the sum of two bf16 to within 2^-17 of itself: hi the nearest, lo the nearest to what is left.  One bf16 alone would be off by up
-// to 2^-8, a rounding of a 32-bit sum that nothing asks for; the second matrix instruction that lo takes is hidden under the memory traffic.
-__device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& lo) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int p = 0; p < 4; p++) {
-    h[p] = bf16_rne_pack(x[2 * p], x[2 * p + 1]);
-    l[p] = bf16_rne_pack(x[2 * p] - bf16lo_f32(h[p]), x[2 * p + 1] - bf16hi_f32(h[p]));
-  }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(l[0], l[1], l[2], l[3]);
-}
-// The same in three parts, exact to the last bit of the float: what the weight gradients take, whose float32 results would show 2^-17.
+// A float as the sum of bf16.  One alone would be off by up to 2^-8, a rounding of a 32-bit sum that nothing asks for; the matrix instructions that the
+// others take are hidden under the memory traffic.  hi (the nearest) and lo (the nearest to what is left) are off by at most 2^-17, which the bf16 results
+// of `up` do not show; with a third part nothing is lost, for the weight gradients, whose float32 results would.
 __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& mid, uint4& lo) {
   uint32_t h[4], m[4], l[4];
 #pragma unroll
@@ -109,249 +105,505 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& mi
   mid = make_uint4(m[0], m[1], m[2], m[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
-// Transposes an 8 x 8 block of 16-bit elements held by one lane: x[i] holds elements (i, 0..7); out[j] holds (0..7, j).
-__device__ __forceinline__ void transpose8(const uint4 (&x)[8], uint4 (&out)[8]) {
-  const uint32_t* s = (const uint32_t*)x;
-  uint32_t* d = (uint32_t*)out;
+// Transposes a block of eight rows of eight 16-bit elements held by one lane: b[j] holds rows 0 .. 7 of element j.
+__device__ __forceinline__ void transpose_rows(const uint32_t (&x)[8][4], uint4 (&b)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; j++)
-#pragma unroll
-    for (int p = 0; p < 4; p++)
-      d[j * 4 + p] = __builtin_amdgcn_perm(s[(2 * p + 1) * 4 + (j >> 1)], s[2 * p * 4 + (j >> 1)], (j & 1) ? 0x07060302u : 0x05040100u);
+  for (int j = 0; j < 8; j++) {
+    const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+    const int k = j >> 1;
+    b[j] = make_uint4(__builtin_amdgcn_perm(x[1][k], x[0][k], sel), __builtin_amdgcn_perm(x[3][k], x[2][k], sel), __builtin_amdgcn_perm(x[5][k], x[4][k], sel),
+                      __builtin_amdgcn_perm(x[7][k], x[6][k], sel));
+  }
 }
 
-// ---- down -----------------------------------------------------------------------------------------------------
-// A workgroup takes 16 TT rows of one adapter, its waves the contraction in turn (64 elements a step: lane quarter q holds elements 16 q ..
-// 16 q + 15, eight of them per matrix instruction, the same on both operands), so that every element of X and of the adapter is read once
-// per workgroup; the waves' sums meet in LDS in a fixed order.
-template <int DT, int RT, int TT, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64)
-k_adapter_down(AdapterSegments g, const uint8_t* __restrict__ X, int64_t ldx, int K, const uint16_t* __restrict__ W, int64_t ldw, int R,
-               const float* __restrict__ scale, float x_scale, float* __restrict__ D, int64_t ldd) {
-  constexpr int RP = RT * 16, TR = TT * 16, LD = RP + 4, EB = DT == M_BF16 ? 2 : 1;
-  __shared__ float red[WAVES][TR][LD];
-  const Tile t = find_tile(g, blockIdx.x, TR);
-  if (t.rows <= 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (t.adapter < 0) {
-    for (int i = tid; i < t.rows * (R / 4); i += WAVES * 64) {
-      const int row = i / (R / 4), c = i - row * (R / 4);
-      *(float4*)(D + (t.row + row) * ldd + c * 4) = make_float4(0, 0, 0, 0);
-    }
-    return;
-  }
-  const int m = lane & 15, q = lane >> 4;
-  const uint8_t* xp[TT];
-#pragma unroll
-  for (int i = 0; i < TT; i++) xp[i] = X + ((t.row + min(i * 16 + m, t.rows - 1)) * ldx + 16 * q) * EB;
-  const uint16_t* wp[RT];
-#pragma unroll
-  for (int i = 0; i < RT; i++) wp[i] = W + ((int64_t)t.adapter * R + min(i * 16 + m, R - 1)) * ldw + 16 * q;
+// ---- guarded memory -------------------------------------------------------------------------------------------
+// Rows and elements that a tile does not have are left to the descriptor's range check: loads give zeros, stores nothing, without a branch around each
+// (a branch a load costs more registers than it saves, since the loads can no longer be moved together).  A descriptor covers a tile's rows of one
+// matrix, at most 2^31 bytes (leading dimensions are at most 2^23), so an offset of kNowhere lies behind every one.
+constexpr uint32_t kNowhere = 0x80000000u;
+template <class T>
+__device__ __forceinline__ BufferRsrc rows_of(const T* base, int64_t first, int rows, int64_t ld, int width) {
+  return make_rsrc(base + first * ld, rows > 0 && base ? ((uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)width) * (uint32_t)sizeof(T) : 0u);
+}
+__device__ __forceinline__ void buffer_store_b128(BufferRsrc r, uint32_t voffset, uint4 v) {
+  i32x4 t;
+  __builtin_memcpy(&t, &v, 16);
+  __builtin_amdgcn_raw_buffer_store_b128(t, r, (int)voffset, 0, 0);
+}
 
-  f32x4 acc[RT][TT];
-#pragma unroll
-  for (int i = 0; i < RT; i++)
-#pragma unroll
-    for (int j = 0; j < TT; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
+// ---- down and up ----------------------------------------------------------------------------------------------
+// Down, for 16 TT rows of one adapter and the contraction's elements k0 .. k1 - 1, by a workgroup of eight waves: KC elements at a time go through LDS,
+// of the rows and of the adapter, loaded in whole pieces of a row (the operands' own layout has a different row in every lane, at a quarter of the load
+// rate) and kept two chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
+// waves, the waves share the tile's rows and ranks out as well.  The sums of the steps' waves meet in LDS, in the order of the steps.
+template <int DT, int RT, int TT>
+struct Down {
+  static constexpr int RP = RT * 16, TR = TT * 16, EB = DT == M_BF16 ? 2 : 1;
+  static constexpr int KC = RP <= 32 ? 256 : 8192 / RP, STEPS = KC / 32, GROUPS = 8 / STEPS;       // a chunk, its steps, the waves that share a step
+  static constexpr int GT = GROUPS < TT ? GROUPS : TT, GR = GROUPS / GT, TW = TT / GT, RW = RT / GR;   // shares by rows and by ranks, a wave's own tiles
+  static constexpr int LDK = KC + 8, LD = RP + 4;                                                  // LDS rows start four banks apart
+  static constexpr int PC = KC / 8, XP = (TR * PC + 511) / 512, WP = (RP * PC + 511) / 512;        // pieces of eight elements: of a row, a thread's
+  static constexpr int STAGE = (TR + RP) * LDK * 2, RED = STEPS * TR * LD * 4, LDS = 2 * STAGE > RED ? 2 * STAGE : RED;
+  template <bool BITS8> struct Raw { using T = uint4; };
+  template <> struct Raw<true> { using T = uint2; };
+  struct Chunk { typename Raw<DT != M_BF16>::T x[XP]; uint4 w[WP]; };
 
-  for (int k = wave * 64; k < K; k += WAVES * 64) {
-    // K is a multiple of 8 (16 in 8 bits): a lane's pieces of eight lie inside the row or behind it
-    const bool in0 = k + 16 * q < K, in1 = k + 16 * q + 8 < K;
-    uint4 x[TT][2], w[RT][2];
+  // Leaves the steps' sums in lds as float [STEPS][TR][LD], behind a barrier.
+  static __device__ __forceinline__ void run(uint8_t* lds, const Tile& t, const uint8_t* __restrict__ X, int64_t ldx, int K, int k0, int k1, const uint16_t* __restrict__ W, int64_t ldw, int R) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
+    const int step = wave % STEPS, t0 = (wave / STEPS) % GT * TW, r0 = (wave / STEPS) / GT * RW;
+    f32x4 acc[RW][TW];
 #pragma unroll
-    for (int i = 0; i < TT; i++) {
-      if (DT == M_BF16) {
-        x[i][0] = load16(xp[i] + k * 2, in0);
-        x[i][1] = load16(xp[i] + k * 2 + 16, in1);
-      } else {
-        const uint4 c = load16(xp[i] + k, in0);
-        x[i][0] = widen<DT>(make_uint2(c.x, c.y), 1.0f);
-        x[i][1] = widen<DT>(make_uint2(c.z, c.w), 1.0f);
+    for (int i = 0; i < RW; i++)
+#pragma unroll
+      for (int j = 0; j < TW; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
+    // Rows behind the tile's, ranks behind R and elements behind k1 are zeros; nothing is read for them.
+    const BufferRsrc rx = make_rsrc(X + t.row * ldx * EB, ((uint32_t)(t.rows - 1) * (uint32_t)ldx + (uint32_t)K) * EB);
+    const BufferRsrc rw = rows_of(W, (int64_t)t.adapter * R, R, ldw, K);
+    auto load = [&](Chunk& c, int k) {
+#pragma unroll
+      for (int i = 0; i < XP; i++) {
+        const int p = i * 512 + tid, r = p / PC, e = k + p % PC * 8;
+        const uint32_t at = e < k1 ? ((uint32_t)r * (uint32_t)ldx + (uint32_t)e) * EB : kNowhere;
+        if constexpr (DT == M_BF16) c.x[i] = buffer_load_b128(rx, at, 0);
+        else c.x[i] = buffer_load_b64(rx, at, 0);
       }
+#pragma unroll
+      for (int i = 0; i < WP; i++) {
+        const int p = i * 512 + tid, r = p / PC, e = k + p % PC * 8;
+        c.w[i] = buffer_load_b128(rw, e < k1 ? ((uint32_t)r * (uint32_t)ldw + (uint32_t)e) * 2 : kNowhere, 0);
+      }
+    };
+    auto put = [&](const Chunk& c, int buffer) {
+      uint8_t* to = lds + buffer * STAGE;
+#pragma unroll
+      for (int i = 0; i < XP; i++) {
+        const int p = i * 512 + tid, r = p / PC;
+        if (TR * PC % 512 != 0 && r >= TR) continue;
+        uint4* d = (uint4*)(to + (r * LDK + p % PC * 8) * 2);
+        if constexpr (DT == M_BF16) *d = c.x[i];
+        else *d = widen<DT>(c.x[i], 1.0f);
+      }
+#pragma unroll
+      for (int i = 0; i < WP; i++) {
+        const int p = i * 512 + tid, r = p / PC;
+        if (RP * PC % 512 == 0 || r < RP) *(uint4*)(to + ((TR + r) * LDK + p % PC * 8) * 2) = c.w[i];
+      }
+    };
+    auto multiply = [&](int buffer) {
+      const uint16_t* from = (const uint16_t*)(lds + buffer * STAGE) + step * 32 + q * 8;
+      uint4 x[TW];
+#pragma unroll
+      for (int j = 0; j < TW; j++) x[j] = *(const uint4*)(from + ((t0 + j) * 16 + m) * LDK);
+#pragma unroll
+      for (int i = 0; i < RW; i++) {
+        const uint4 w = *(const uint4*)(from + (TR + (r0 + i) * 16 + m) * LDK);
+#pragma unroll
+        for (int j = 0; j < TW; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(w), frag(x[j]), acc[i][j], 0, 0, 0);
+      }
+    };
+    Chunk a, b;
+    load(a, k0);
+    load(b, k0 + KC);
+    for (int k = k0; k < k1; k += 2 * KC) {            // a chunk behind k1 is zeros
+      put(a, 0);
+      __syncthreads();
+      load(a, k + 2 * KC);
+      multiply(0);
+      put(b, 1);                                       // the barrier before it is behind the last reads of this buffer
+      __syncthreads();
+      load(b, k + 3 * KC);
+      multiply(1);
     }
+    __syncthreads();
+    // lane (m, q) holds ranks 4 q .. 4 q + 3 of row m
+    float (*red)[TR][LD] = (float (*)[TR][LD])lds;
 #pragma unroll
-    for (int i = 0; i < RT; i++) {
-      w[i][0] = load16(wp[i] + k, in0);
-      w[i][1] = load16(wp[i] + k + 8, in1);
-    }
+    for (int i = 0; i < RW; i++)
 #pragma unroll
-    for (int h = 0; h < 2; h++)
-#pragma unroll
-      for (int i = 0; i < RT; i++)
-#pragma unroll
-        for (int j = 0; j < TT; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(w[i][h]), frag(x[j][h]), acc[i][j], 0, 0, 0);
+      for (int j = 0; j < TW; j++) *(f32x4*)&red[step][(t0 + j) * 16 + m][(r0 + i) * 16 + 4 * q] = acc[i][j];
+    __syncthreads();
   }
-  // lane (m, q) holds ranks 4 q .. 4 q + 3 of row m
-#pragma unroll
-  for (int i = 0; i < RT; i++)
-#pragma unroll
-    for (int j = 0; j < TT; j++) *(f32x4*)&red[wave][j * 16 + m][i * 16 + 4 * q] = acc[i][j];
-  __syncthreads();
-  const float s = (scale ? scale[t.adapter] : 1.0f) * x_scale;
-  for (int i = tid; i < t.rows * (RP / 4); i += WAVES * 64) {
-    const int row = i / (RP / 4), c = (i % (RP / 4)) * 4;
-    if (c >= R) continue;
+  // Ranks c .. c + 3 of a row
+  static __device__ __forceinline__ f32x4 sum(const uint8_t* lds, int row, int c) {
+    const float (*red)[TR][LD] = (const float (*)[TR][LD])lds;
     f32x4 v = *(const f32x4*)&red[0][row][c];
 #pragma unroll
-    for (int u = 1; u < WAVES; u++) v += *(const f32x4*)&red[u][row][c];
-    *(f32x4*)(D + (t.row + row) * ldd + c) = v * s;
+    for (int u = 1; u < STEPS; u++) v += *(const f32x4*)&red[u][row][c];
+    return v;
   }
-}
+};
 
-// ---- up -------------------------------------------------------------------------------------------------------
-// A wave takes 128 features and walks the tile's rows 16 at a time.  Lane (n, q) holds eight neighbouring features of ranks 8 q .. 8 q + 7, in
-// registers for all rows: eight loads of 16 bytes, transposed in registers, are the operands of eight matrix instructions, the j-th for features
-// 8 n + j, so that the results of one row lie 8 in a lane and 128 in 16 lanes, 256 bytes in a row of base and out.
-template <int RP, int TR>
-__global__ void __launch_bounds__(256)
-k_adapter_up(AdapterSegments g, const float* __restrict__ D, int64_t ldd, int R, const uint16_t* __restrict__ U, int64_t ldu, int C, int fblocks,
-             const uint16_t* base, int64_t ldbase, uint16_t* out, int64_t ldout) {
-  constexpr int SETS = RP <= 32 ? 1 : RP / 32;
-  const int slot = blockIdx.x / fblocks, fb = blockIdx.x - slot * fblocks;
-  const Tile t = find_tile(g, slot, TR);
-  if (t.rows <= 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, q = lane >> 4, f = (fb * 4 + wave) * 128 + n * 8;
-  const bool in = f < C;
-  if (t.adapter < 0) {
-    if (out == base || !in) return;
-    for (int r = q; r < t.rows; r += 4)
-      *(uint4*)(out + (t.row + r) * ldout + f) = load16(base + (t.row + r) * ldbase + f, base != nullptr);
-    return;
-  }
-  uint4 b[SETS][8];
-#pragma unroll
-  for (int s = 0; s < SETS; s++) {
-    uint4 x[8];
+constexpr int kMostSplits = 4;      // of the contraction of `down`
+
+struct DownArgs {
+  const uint8_t* X;
+  int64_t ldx;
+  int K;
+  const uint16_t* W;
+  int64_t ldw;
+  int R;
+  const float* scale;
+  float x_scale;
+  float* D;
+  int64_t ldd;
+};
+struct UpArgs {
+  const uint16_t* U;
+  int64_t ldu;
+  int C;
+  const uint16_t* base;
+  int64_t ldbase;
+  uint16_t* out;
+  int64_t ldout;
+};
+
+// A tile's rows of D as the sum of two bf16, and the features of a wave.
+template <int RP, int TT>
+struct Up {
+  static constexpr int TR = TT * 16, LDP = RP + 8, SETS = RP <= 32 ? 1 : RP / 32;
+  uint16_t parts[2][TR][LDP];
+
+  // What a wave loads of its features before it needs the tile's D: the first 32 ranks of the adapter, and its rows of base.
+  struct Ahead {
+    uint32_t x[8][4];
+    uint4 old[TT][4];
+  };
+  static __device__ __forceinline__ void load_ranks(uint32_t (&x)[8][4], int s, BufferRsrc ru, int64_t ldu, uint32_t at) {
+    const int q = ((int)threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      const int r = (RP == 16 ? (q & 1) * 8 : s * 32 + q * 8) + i;
-      x[i] = load16(U + ((int64_t)t.adapter * R + r) * ldu + f, in && r < R);
+      const uint32_t r = (RP == 16 ? (q & 1) * 8 : s * 32 + q * 8) + i;
+      const uint4 v = buffer_load_b128(ru, at + r * (uint32_t)ldu * 2, 0);
+      x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
     }
-    transpose8(x, b[s]);
   }
-  for (int r0 = 0; r0 < t.rows; r0 += 16) {
-    uint4 old[4];
+  static __device__ __forceinline__ void load(Ahead& a, const Tile& t, int f0, const UpArgs& o, int R) {
+    const int lane = threadIdx.x & 63, q = lane >> 4, f = f0 + (lane & 15) * 8;
+    const uint32_t at = f < o.C ? (uint32_t)f * 2 : kNowhere;
+    load_ranks(a.x, 0, rows_of(o.U, (int64_t)t.adapter * R, R, o.ldu, o.C), o.ldu, at);
+    const BufferRsrc rb = rows_of(o.base, t.row, t.rows, o.ldbase, o.C);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int r = r0 + 4 * q + i;
-      old[i] = load16(base + (t.row + r) * ldbase + f, base && in && r < t.rows);
-    }
-    f32x4 acc[8];
+    for (int j = 0; j < TT; j++)
 #pragma unroll
-    for (int j = 0; j < 8; j++) acc[j] = (f32x4){0, 0, 0, 0};
-    const float* d = D + (t.row + min(r0 + n, t.rows - 1)) * ldd;
+      for (int i = 0; i < 4; i++) a.old[j][i] = buffer_load_b128(rb, at + (uint32_t)(j * 16 + 4 * q + i) * (uint32_t)o.ldbase * 2, 0);
+  }
+  __device__ __forceinline__ void put(int row, int c, f32x4 v) {
+    uint2 hi, lo;
+    hi.x = bf16_rne_pack(v[0], v[1]);
+    hi.y = bf16_rne_pack(v[2], v[3]);
+    lo.x = bf16_rne_pack(v[0] - bf16lo_f32(hi.x), v[1] - bf16hi_f32(hi.x));
+    lo.y = bf16_rne_pack(v[2] - bf16lo_f32(hi.y), v[3] - bf16hi_f32(hi.y));
+    *(uint2*)&parts[0][row][c] = hi;
+    *(uint2*)&parts[1][row][c] = lo;
+  }
+  // Features f0 .. f0 + 127.  Lane (m, q) loads eight neighbouring features of ranks 8 q .. 8 q + 7 in eight pieces of 16 bytes and transposes them in
+  // registers: the operands of eight matrix instructions, the j-th for features 8 m + j, so that the results of one row lie 8 in a lane and 128 in 16
+  // lanes, 256 bytes in a row of base and out.
+  __device__ __forceinline__ void run(Ahead& a, const Tile& t, int f0, const UpArgs& o, int R) const {
+    const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4, f = f0 + m * 8;
+    const uint32_t at = f < o.C ? (uint32_t)f * 2 : kNowhere;
+    const BufferRsrc ru = rows_of(o.U, (int64_t)t.adapter * R, R, o.ldu, o.C), ro = rows_of((const uint16_t*)o.out, t.row, t.rows, o.ldout, o.C);
+    f32x4 sum[SETS == 1 ? 1 : TT][8];                    // of one set of ranks the rows are finished 16 at a time
 #pragma unroll
     for (int s = 0; s < SETS; s++) {
-      const int r = RP == 16 ? (q & 1) * 8 : s * 32 + q * 8;
-      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (r < R) {
-        const float4 u = *(const float4*)(d + r), v = *(const float4*)(d + r + 4);
-        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-      }
-      uint4 hi, lo;
-      split8(x, hi, lo);
-      if (RP == 16) {                                  // hi and lo of 16 ranks fill one instruction's 32 places
-        const uint4 a = q < 2 ? hi : lo;
+      uint4 u[8];
+      transpose_rows(a.x, u);
+      if (s + 1 < SETS) load_ranks(a.x, s + 1, ru, o.ldu, at);
 #pragma unroll
-        for (int j = 0; j < 8; j++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(a), frag(b[s][j]), acc[j], 0, 0, 0);
-      } else {
+      for (int k = 0; k < TT; k++) {
+        f32x4 (&c)[8] = sum[SETS == 1 ? 0 : k];
+        if (s == 0)
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(b[s][j]), acc[j], 0, 0, 0);
-          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(b[s][j]), acc[j], 0, 0, 0);
+          for (int j = 0; j < 8; j++) c[j] = (f32x4){0, 0, 0, 0};
+        if (RP == 16) {                                  // hi and lo of 16 ranks fill one instruction's 32 places
+          const uint4 d = *(const uint4*)&parts[q >> 1][k * 16 + m][(q & 1) * 8];
+#pragma unroll
+          for (int j = 0; j < 8; j++) c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(d), frag(u[j]), c[j], 0, 0, 0);
+        } else {
+          const uint4 hi = *(const uint4*)&parts[0][k * 16 + m][s * 32 + q * 8], lo = *(const uint4*)&parts[1][k * 16 + m][s * 32 + q * 8];
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(u[j]), c[j], 0, 0, 0);
+            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(u[j]), c[j], 0, 0, 0);
+          }
+        }
+        if (s + 1 < SETS) continue;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const uint4 old = a.old[k][i];
+          uint4 v;
+          v.x = bf16_rne_pack(bf16lo_f32(old.x) + c[0][i], bf16hi_f32(old.x) + c[1][i]);
+          v.y = bf16_rne_pack(bf16lo_f32(old.y) + c[2][i], bf16hi_f32(old.y) + c[3][i]);
+          v.z = bf16_rne_pack(bf16lo_f32(old.z) + c[4][i], bf16hi_f32(old.z) + c[5][i]);
+          v.w = bf16_rne_pack(bf16lo_f32(old.w) + c[6][i], bf16hi_f32(old.w) + c[7][i]);
+          buffer_store_b128(ro, at + (uint32_t)(k * 16 + 4 * q + i) * (uint32_t)o.ldout * 2, v);
         }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int r = r0 + 4 * q + i;
-      if (!in || r >= t.rows) continue;
-      uint4 v;
-      v.x = bf16_rne_pack(bf16lo_f32(old[i].x) + acc[0][i], bf16hi_f32(old[i].x) + acc[1][i]);
-      v.y = bf16_rne_pack(bf16lo_f32(old[i].y) + acc[2][i], bf16hi_f32(old[i].y) + acc[3][i]);
-      v.z = bf16_rne_pack(bf16lo_f32(old[i].z) + acc[4][i], bf16hi_f32(old[i].z) + acc[5][i]);
-      v.w = bf16_rne_pack(bf16lo_f32(old[i].w) + acc[6][i], bf16hi_f32(old[i].w) + acc[7][i]);
-      *(uint4*)(out + (t.row + r) * ldout + f) = v;
-    }
+  }
+};
+
+// Rows without an adapter: D is zero, out is base
+__device__ __forceinline__ void bare_rows(const Tile& t, float* D, int64_t ldd, int R) {
+  for (int i = threadIdx.x; i < t.rows * (R / 4); i += blockDim.x) {
+    const int row = i / (R / 4), c = i - row * (R / 4);
+    *(float4*)(D + (t.row + row) * ldd + c * 4) = make_float4(0, 0, 0, 0);
+  }
+}
+__device__ __forceinline__ void bare_features(const Tile& t, int f0, int C, const uint16_t* base, int64_t ldbase, uint16_t* out, int64_t ldout) {
+  const int lane = threadIdx.x & 63, f = f0 + (lane & 15) * 8;
+  if (out == base || f >= C) return;
+  for (int r = lane >> 4; r < t.rows; r += 4) *(uint4*)(out + (t.row + r) * ldout + f) = load16(base + (t.row + r) * ldbase + f, base != nullptr);
+}
+
+__device__ __forceinline__ float scale_of(const DownArgs& a, const Tile& t) { return (a.scale ? a.scale[t.adapter] : 1.0f) * a.x_scale; }
+
+// Both products of 16 rows in one launch, for few rows: `slices` workgroups share a tile's features, and each computes D for itself.
+template <int DT, int RT>
+__global__ void __launch_bounds__(512)
+k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, int slices) {
+  using D = Down<DT, RT, 1>;
+  __shared__ __align__(16) uint8_t lds[D::LDS];
+  __shared__ __align__(16) Up<RT * 16, 1> up;
+  const int slot = (int)blockIdx.x / slices, slice = (int)blockIdx.x - slot * slices;
+  const Tile t = find_tile(g, slot, 16);
+  if (t.rows <= 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  if (t.adapter < 0) {
+    if (slice == 0) bare_rows(t, d.D, d.ldd, d.R);
+    for (int f = (slice * 8 + wave) * 128; f < o.C; f += slices * 1024) bare_features(t, f, o.C, o.base, o.ldbase, o.out, o.ldout);
+    return;
+  }
+  const float s = scale_of(d, t);
+  D::run(lds, t, d.X, d.ldx, d.K, 0, d.K, d.W, d.ldw, d.R);
+  for (int i = threadIdx.x; i < 16 * RT * 4; i += 512) {
+    const int row = i / (RT * 4), c = i % (RT * 4) * 4;
+    f32x4 v = D::sum(lds, row, c) * s;
+    if (c >= d.R) v = (f32x4){0, 0, 0, 0};                                       // ranks of the padding, where s may be anything
+    if (slice == 0 && row < t.rows && c < d.R) *(f32x4*)(d.D + (t.row + row) * d.ldd + c) = v;
+    up.put(row, c, v);
+  }
+  __syncthreads();
+  for (int f = (slice * 8 + wave) * 128; f < o.C; f += slices * 1024) {
+    typename Up<RT * 16, 1>::Ahead a;
+    up.load(a, t, f, o, d.R);
+    up.run(a, t, f, o, d.R);
   }
 }
 
+// Down alone.  splits > 1: `splits` workgroups share a tile's contraction, `span` elements each, and leave their sums, unscaled, in part[split][row][rank].
+template <int DT, int RT, int TT>
+__global__ void __launch_bounds__(512)
+k_adapter_down(AdapterSegments g, DownArgs d, int splits, int span, float* __restrict__ part) {
+  using D = Down<DT, RT, TT>;
+  __shared__ __align__(16) uint8_t lds[D::LDS];
+  const int slot = (int)blockIdx.x / splits, split = (int)blockIdx.x - slot * splits;
+  const Tile t = find_tile(g, slot, TT * 16);
+  if (t.rows <= 0) return;
+  if (t.adapter < 0) {
+    if (split == 0) bare_rows(t, d.D, d.ldd, d.R);
+    return;
+  }
+  const float s = splits > 1 ? 1.0f : scale_of(d, t);
+  D::run(lds, t, d.X, d.ldx, d.K, split * span, min(d.K, (split + 1) * span), d.W, d.ldw, d.R);
+  float* to = splits > 1 ? part + ((int64_t)split * g.T + t.row) * d.R : d.D + t.row * d.ldd;
+  const int64_t ld = splits > 1 ? d.R : d.ldd;
+  for (int i = threadIdx.x; i < t.rows * (RT * 4); i += 512) {
+    const int row = i / (RT * 4), c = i % (RT * 4) * 4;
+    if (c < d.R) *(f32x4*)(to + row * ld + c) = D::sum(lds, row, c) * s;
+  }
+}
+
+// Up alone, 512 features of a tile's rows in a workgroup of four waves.  splits > 1: adds the splits' sums in order and scales them; the workgroups of
+// the first features write D.
+template <int RP, int TT>
+__global__ void __launch_bounds__(256, RP <= 32 ? 3 : 2)
+k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, int fblocks, int splits, const float* __restrict__ part) {
+  __shared__ __align__(16) Up<RP, TT> up;
+  const int slot = (int)blockIdx.x / fblocks, fb = (int)blockIdx.x - slot * fblocks;
+  const Tile t = find_tile(g, slot, TT * 16);
+  if (t.rows <= 0) return;
+  const int f = (fb * 4 + ((int)threadIdx.x >> 6)) * 128;
+  if (t.adapter < 0) {
+    bare_features(t, f, o.C, o.base, o.ldbase, o.out, o.ldout);
+    return;
+  }
+  typename Up<RP, TT>::Ahead a;
+  up.load(a, t, f, o, d.R);
+  const float s = splits > 1 ? scale_of(d, t) : 1.0f;
+  const float* from = splits > 1 ? part + t.row * d.R : d.D + t.row * d.ldd;
+  const int64_t ld = splits > 1 ? d.R : d.ldd;
+  for (int i = threadIdx.x; i < TT * RP * 4; i += 256) {
+    const int row = i / (RP / 4), c = i % (RP / 4) * 4;
+    f32x4 v = {0, 0, 0, 0};
+    if (row < t.rows && c < d.R) {
+      v = *(const f32x4*)(from + row * ld + c);
+      if (splits > 1) {
+        f32x4 more[kMostSplits - 1];                   // all under way at once
+#pragma unroll
+        for (int k = 1; k < kMostSplits; k++) {
+          more[k - 1] = (f32x4){0, 0, 0, 0};
+          if (k < splits) more[k - 1] = *(const f32x4*)(from + ((int64_t)k * g.T + row) * d.R + c);
+        }
+#pragma unroll
+        for (int k = 1; k < kMostSplits; k++) v += more[k - 1];
+        v *= s;
+        if (fb == 0) *(f32x4*)(d.D + (t.row + row) * d.ldd + c) = v;
+      }
+    }
+    up.put(row, c, v);
+  }
+  __syncthreads();
+  if (f < o.C) up.run(a, t, f, o, d.R);
+}
+
 // ---- outer ----------------------------------------------------------------------------------------------------
-// A workgroup takes 128 features of a chunk of rows of one segment, its four waves 32 rows each in turn.  Lane (n, q) loads eight features of
-// rows 8 q .. 8 q + 7 (256 bytes of a row in 16 lanes) and transposes them in registers into the operands of eight matrix instructions, as above.
-// The waves' sums meet in LDS; the chunk's sum goes to the workspace, and k_adapter_outer_sum adds the chunks of each adapter in order.
-template <int MT, int RT>
-__global__ void __launch_bounds__(256)
-k_adapter_outer(AdapterSegments g, const float* __restrict__ L, int64_t ldl, int R, const uint8_t* __restrict__ M, int64_t ldm, const uint8_t* __restrict__ blocks,
-                int64_t ldblocks, int C, int fblocks, int chunk, float* __restrict__ part) {
-  constexpr int EB = MT == M_BF16 ? 2 : 1;
-  __shared__ float red[4][16][132];
-  const int slot = blockIdx.x / fblocks, fb = blockIdx.x - slot * fblocks;
+// A workgroup of four waves takes 512 features of a chunk of rows of one segment, 128 in a wave, and up to 64 ranks, 32 rows at a time.  Lane (n, q) loads eight features of rows
+// 8 q .. 8 q + 7 (256 bytes of a row in 16 lanes), one step ahead, and transposes them in registers into the operands of eight matrix instructions.
+// L is split into its three parts once per workgroup: each wave prepares one of the operands and leaves it in LDS for the others.
+// The chunk's sum goes to the workspace, and k_adapter_outer_sum adds the chunks of each adapter in order.
+// Both weight gradients are one launch, the workgroups of X before those of dZ.  With more than 64 ranks two workgroups work on the same rows and features,
+// eight apart in the grid, which is the same XCD: the second finds them in its L2.
+struct OuterArgs {
+  const float* L;
+  int64_t ldl;
+  const uint8_t* M;
+  int64_t ldm;
+  int type;
+  const uint8_t* blocks;
+  int64_t ldblocks;
+  int C, fblocks;
+  float* part;
+};
+// Raw elements of eight rows, eight features of each, and a checkpoint's scale bytes; and the same as operands.
+template <bool BITS8>
+struct OuterRows {
+  static constexpr int WORDS = BITS8 ? 2 : 4;
+  uint32_t x[8][WORDS];
+  uint32_t e[BITS8 ? 8 : 1];
+
+  static __device__ __forceinline__ void words(uint32_t (&to)[WORDS], BufferRsrc r, uint32_t at) {
+    if constexpr (BITS8) {
+      const uint2 v = buffer_load_b64(r, at, 0);
+      to[0] = v.x, to[1] = v.y;
+    } else {
+      const uint4 v = buffer_load_b128(r, at, 0);
+      to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+    }
+  }
+  // `f`: the lane's features, or kNowhere
+  __device__ __forceinline__ void load(const OuterArgs& a, const Tile& t, int r0, uint32_t f) {
+    const uint32_t q = ((uint32_t)threadIdx.x & 63) >> 4;
+    const int rows = min(t.rows - r0, 32);
+    const BufferRsrc r = BITS8 ? rows_of(a.M, t.row + r0, rows, a.ldm, a.C) : rows_of((const uint16_t*)a.M, t.row + r0, rows, a.ldm, a.C);
+#pragma unroll
+    for (int i = 0; i < 8; i++) words(x[i], r, f == kNowhere ? f : ((q * 8 + i) * (uint32_t)a.ldm + f) * (BITS8 ? 1 : 2));
+    if constexpr (BITS8) {
+      const BufferRsrc rs = rows_of(a.type == M_BLOCK ? a.blocks : nullptr, t.row + r0, rows, a.ldblocks, (a.C + 31) / 32);
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        e[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(f == kNowhere ? f : (q * 8 + i) * (uint32_t)a.ldblocks + (f >> 5)), 0, 0);
+    }
+  }
+  // b[j]: rows 0 .. 7 of feature j
+  __device__ __forceinline__ void operands(uint4 (&b)[8], int type) const {
+    if constexpr (!BITS8) transpose_rows(x, b);
+    else {
+      uint32_t w[8][4];
+      const bool e5m2 = type == M_E5M2, blocks = type == M_BLOCK;
+      if (e5m2) {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+          for (int k = 0; k < 2; k++) widen4<M_E5M2>(w[i][2 * k], w[i][2 * k + 1], x[i][k], 1.0f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+          for (int k = 0; k < 2; k++) widen4<M_E4M3>(w[i][2 * k], w[i][2 * k + 1], x[i][k], u2f(blocks ? e[i] << 23 : 0x3F800000u));
+      }
+      transpose_rows(w, b);
+    }
+  }
+};
+template <int RT>
+struct Outer {
+  static_assert(RT <= 4, "a wave prepares one operand of L");
+  static constexpr int LDS = 2 * RT * 3 * 64 * 16;
+
+  template <bool BITS8>
+  static __device__ __forceinline__ void run(uint8_t* lds, const OuterArgs& a, const Tile& t, int slot, int fb, int rank0, int R) {
+    uint4 (*l)[RT][3][64] = (uint4 (*)[RT][3][64])lds;                             // [buffer][ranks][part][lane]
+    const int lane = (int)threadIdx.x & 63, fw = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n = lane & 15, q = lane >> 4, f = (fb * 4 + fw) * 128 + n * 8;
+    const bool in = f < a.C;
+    const uint32_t at = in ? (uint32_t)f : kNowhere;
+    const int mine = rank0 + fw * 16 + n;                                          // the rank of L that this lane prepares
+    f32x4 acc[RT][8];
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+      for (int j = 0; j < 8; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
+
+    float v[8];
+    auto load_l = [&](int r0) {
+      const BufferRsrc r = rows_of(a.L, t.row + r0, min(t.rows - r0, 32), a.ldl, R);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = u2f((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)(fw < RT && mine < R ? ((uint32_t)(q * 8 + e) * (uint32_t)a.ldl + (uint32_t)mine) * 4 : kNowhere), 0, 0));
+    };
+    OuterRows<BITS8> m;
+    load_l(0);
+    m.load(a, t, 0, at);
+    int buffer = 0;
+    for (int r0 = 0; r0 < t.rows; r0 += 32, buffer ^= 1) {
+      if (fw < RT) split8(v, l[buffer][fw][0][lane], l[buffer][fw][1][lane], l[buffer][fw][2][lane]);
+      __syncthreads();                                 // nobody comes here before it has read the other buffer, which is written next
+      uint4 b[8];
+      m.operands(b, a.type);
+      load_l(r0 + 32);
+      m.load(a, t, r0 + 32, at);
+#pragma unroll
+      for (int i = 0; i < RT; i++) {
+        const uint4 hi = l[buffer][i][0][lane], mid = l[buffer][i][1][lane], lo = l[buffer][i][2][lane];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(b[j]), acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(mid), frag(b[j]), acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(b[j]), acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+    // lane (n, q) holds ranks 4 q .. 4 q + 3 of features 8 n .. 8 n + 7
+    if (!in) return;
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int rank = rank0 + i * 16 + 4 * q + e;
+        if (rank >= R) continue;
+#pragma unroll
+        for (int h = 0; h < 8; h += 4)
+          *(f32x4*)(a.part + ((int64_t)slot * R + rank) * a.C + f + h) = (f32x4){acc[i][h][e], acc[i][h + 1][e], acc[i][h + 2][e], acc[i][h + 3][e]};
+      }
+  }
+};
+template <int RT>
+__global__ void __launch_bounds__(256, RT == 1 ? 3 : 2)
+k_adapter_outer(AdapterSegments g, OuterArgs x, OuterArgs z, int R, int chunk) {
+  __shared__ __align__(16) uint8_t lds[Outer<RT>::LDS];
+  const bool pairs = R > 64;
+  const int block = pairs ? (int)blockIdx.x / 16 * 8 + (int)blockIdx.x % 8 : (int)blockIdx.x, rank0 = pairs ? ((int)blockIdx.x / 8 & 1) * 64 : 0;
+  const int fblocks = x.fblocks + z.fblocks, slot = block / fblocks;
+  if (slot >= g.T / chunk + g.segments + 2) return;                                // the last pairs may be empty
+  int fb = block - slot * fblocks;
+  const bool second = fb >= x.fblocks;
+  const OuterArgs a = second ? z : x;
+  if (second) fb -= x.fblocks;
   const Tile t = find_tile(g, slot, chunk);
   if (t.rows <= 0 || t.adapter < 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, q = lane >> 4, f = fb * 128 + n * 8;
-  const bool in = f < C;
-  f32x4 acc[RT][8];
-#pragma unroll
-  for (int i = 0; i < RT; i++)
-#pragma unroll
-    for (int j = 0; j < 8; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
-  for (int r0 = wave * 32; r0 < t.rows; r0 += 128) {
-    uint4 x[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const int r = r0 + q * 8 + i;
-      const bool ok = in && r < t.rows;
-      const uint8_t* p = M + ((t.row + r) * ldm + f) * EB;
-      if (MT == M_BF16) x[i] = load16(p, ok);
-      else {
-        const uint2 c = load8(p, ok);
-        float s = 1.0f;
-        if (MT == M_BLOCK && ok) s = u2f((uint32_t)blocks[(t.row + r) * ldblocks + (f >> 5)] << 23);
-        x[i] = widen<MT>(c, s);
-      }
-    }
-    uint4 b[8];
-    transpose8(x, b);
-#pragma unroll
-    for (int i = 0; i < RT; i++) {
-      float l[8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int r = r0 + q * 8 + e;
-        l[e] = r < t.rows && i * 16 + n < R ? L[(t.row + r) * ldl + i * 16 + n] : 0.0f;
-      }
-      uint4 hi, mid, lo;
-      split8(l, hi, mid, lo);
-#pragma unroll
-      for (int j = 0; j < 8; j++) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(b[j]), acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(mid), frag(b[j]), acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(b[j]), acc[i][j], 0, 0, 0);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < RT; i++) {
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-#pragma unroll
-      for (int h = 0; h < 2; h++)
-        *(f32x4*)&red[wave][4 * q + e][n * 8 + h * 4] = (f32x4){acc[i][h * 4][e], acc[i][h * 4 + 1][e], acc[i][h * 4 + 2][e], acc[i][h * 4 + 3][e]};
-    __syncthreads();
-    for (int u = tid; u < 512; u += 256) {
-      const int r = u >> 5, c = (u & 31) * 4;
-      if (i * 16 + r < R && fb * 128 + c < C) {
-        f32x4 v = *(const f32x4*)&red[0][r][c];
-        v += *(const f32x4*)&red[1][r][c];
-        v += *(const f32x4*)&red[2][r][c];
-        v += *(const f32x4*)&red[3][r][c];
-        *(f32x4*)(part + ((int64_t)slot * R + i * 16 + r) * C + fb * 128 + c) = v;
-      }
-    }
-  }
+  if (a.type == M_BF16) Outer<RT>::template run<false>(lds, a, t, slot, fb, rank0, R);
+  else Outer<RT>::template run<true>(lds, a, t, slot, fb, rank0, R);
 }
 
 struct OuterSum {
@@ -367,16 +619,33 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
   const bool second = (int)blockIdx.x >= ablocks;
   const OuterSum s = second ? b : a;
   const int f = ((int)(second ? blockIdx.x - ablocks : blockIdx.x) * 256 + (int)threadIdx.x) * 4, r = blockIdx.y, n = blockIdx.z;
-  if (f >= s.C) return;
+  const bool in = f < s.C;                             // the lanes stay together for the segments
   f32x4 sum = {0, 0, 0, 0};
-  for (int v = 1; v <= g.segments; v++) {
-    if (g.adapter[v - 1] != n) continue;
-    const int rows = segment_bound(g, v + 1) - segment_bound(g, v);
-    if (rows <= 0) continue;
-    const int first = first_slot(g, v, chunk), last = min(first + (rows - 1) / chunk + 1, first_slot(g, v + 1, chunk));
-#pragma unroll 4
-    for (int k = first; k < last; k++) sum += *(const f32x4*)(s.part + ((int64_t)k * R + r) * s.C + f);
+  const float* from = s.part + (int64_t)r * s.C + f;
+  const int64_t stride = (int64_t)R * s.C;
+  // 64 segments at a time: each lane looks at one, and those of adapter n are worked through in order
+  for (int v0 = 1; v0 <= g.segments; v0 += 64) {
+    const int v = v0 + ((int)threadIdx.x & 63);
+    const int rows = segment_bound(g, v + 1) - segment_bound(g, v), first = first_slot(g, v, chunk);
+    const int last = min(first + (rows - 1) / chunk + 1, first_slot(g, v + 1, chunk));
+    uint64_t todo = __ballot(v <= g.segments && rows > 0 && segment_adapter(g, v) == n);
+    while (todo) {
+      const int lane = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      const int end = __builtin_amdgcn_readlane(last, lane);
+      for (int k = __builtin_amdgcn_readlane(first, lane); k < end; k += 8) {
+        f32x4 part[8];                                 // all under way at once
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          part[i] = (f32x4){0, 0, 0, 0};
+          if (in && k + i < end) part[i] = *(const f32x4*)(from + (k + i) * stride);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum += part[i];
+      }
+    }
   }
+  if (!in) return;
   float* p = s.G + ((int64_t)n * R + r) * s.ldg + f;
   sum *= s.scale;
   if (accumulate) sum += *(const f32x4*)p;
@@ -386,90 +655,126 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
 int mode(int dtype) { return dtype == SSTE_F8E4M3 ? M_E4M3 : dtype == SSTE_F8E5M2 ? M_E5M2 : dtype == SSTE_F8BLOCK ? M_BLOCK : M_BF16; }
 int padded_rank(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
 
-template <int DT, int RP, int TT, int WAVES>
-void down(const AdapterApply& a, hipStream_t s) {
-  SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, TT, WAVES>), dim3((unsigned)slots(a.seg, TT * 16)), dim3(WAVES * 64), s, a.seg, (const uint8_t*)a.X, a.ldx, a.K,
-              (const uint16_t*)a.down, a.lddown, a.R, a.scale, a.x_scale, a.D, a.ldd);
+// How the two products of a call are shared out.  Times are of both kernels, or of the one, in us.
+struct ApplyPlan {
+  bool both;         // one launch
+  int slices;        // of it: workgroups of a tile
+  bool large;        // two launches: tiles of 64 rows for the first, otherwise of 32
+  int splits, span;  // of its contraction
+};
+int apply_chunk(int R) { return padded_rank(R) <= 32 ? 256 : 8192 / padded_rank(R); }      // Down::KC
+ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspace) {
+  ApplyPlan p = {};
+  const int64_t extra = (g.segments < g.T ? g.segments : g.T) + 1;     // tiles that segments, and the rows outside them, may add
+  const int chunk = apply_chunk(R), chunks = (K + chunk - 1) / chunk;
+  // One launch saves one, about 3 us, and does the first product in 16-row tiles without sharing its contraction out.  Rank 16, 1280 -> 3840: 1 row 5.6
+  // against 8.6, 1024 rows 9.2 against 11.2; rank 64, 1280 -> 5120: 512 rows 11.7 against 12.3, 1024 rows 16.7 against 14.9; rank 16, 5120 -> 1280 (20
+  // chunks): 64 rows of two segments 8.5 against 9.1, 256 rows of four 11.6 against 9.2, 256 rows of as many 12.7 against 16.5.
+  const bool single = 2 * (int64_t)g.segments >= g.T;                  // mostly one row a segment: tiles are as good as empty whatever their size
+  p.both = (int64_t)g.T * chunks <= 5120 && (chunks <= 10 || g.T <= 64 || single);
+  if (p.both) {
+    const int64_t tiles = g.T / 16 + extra, passes = (C + 1023) / 1024;
+    p.slices = (int)(1024 / tiles < passes ? 1024 / tiles : passes);
+    if (p.slices < 1) p.slices = 1;
+    return p;
+  }
+  // 64-row tiles read the adapter half as often.  Rank 64, 5120 -> 1280, 16384 rows: 68 against 80, 2999 rows 22.2 against 20.3 (too few tiles); rank 64,
+  // 1024 -> 4096, 8192 rows 44.9 against 44.4 (a short contraction gains nothing); rank 16, 4096 -> 1024, 16384 ragged rows 51 against 46 (a small adapter).
+  const bool wide = padded_rank(R) >= 64;
+  p.large = wide && g.T >= 8192 && (K >= 2048 || g.T >= 32768);
+  // The contraction is shared out, in whole chunks and at least four of them, until there are about 512 workgroups with many ranks, 1024 with few: rank 64,
+  // 2999 ragged rows of 5120: 21.6 in four, 24 in three, 31 in one; rank 16, 16384 ragged rows of 4096: 51 in one, 47 in two, 46 in three.
+  const int64_t tiles = g.T / (p.large ? 64 : 32) + extra;
+  int64_t splits = ((wide ? 512 : 1024) + tiles / 2) / tiles;
+  if (splits > chunks / 4) splits = chunks / 4;
+  if (splits > kMostSplits) splits = kMostSplits;
+  if (splits < 1 || !workspace) splits = 1;
+  p.span = (int)((chunks + splits - 1) / splits * chunk);
+  p.splits = chunks > 0 ? (K + p.span - 1) / p.span : 1;
+  return p;
 }
-template <int RP, int TR>
-void up(const AdapterApply& a, hipStream_t s) {
-  const int fblocks = (a.C + 511) / 512;
-  SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_up<RP, TR>), dim3((unsigned)(slots(a.seg, TR) * fblocks)), dim3(256), s, a.seg, a.D, a.ldd, a.R, (const uint16_t*)a.up, a.ldup, a.C,
-              fblocks, (const uint16_t*)a.base, a.ldbase, (uint16_t*)a.out, a.ldout);
-}
-template <int RP>
+
+template <int DT, int RP>
 void apply(const AdapterApply& a, hipStream_t s) {
-  const bool large = a.seg.T >= 8192;
-  constexpr int TT = RP <= 64 ? 4 : 2, WL = 4, WS = 8;
-  switch (mode(a.dtype)) {
-    case M_BF16: large ? down<M_BF16, RP, TT, WL>(a, s) : down<M_BF16, RP, 1, WS>(a, s); break;
-    case M_E4M3: large ? down<M_E4M3, RP, TT, WL>(a, s) : down<M_E4M3, RP, 1, WS>(a, s); break;
-    default: large ? down<M_E5M2, RP, TT, WL>(a, s) : down<M_E5M2, RP, 1, WS>(a, s); break;
+  const ApplyPlan p = plan_apply(a.seg, a.R, a.K, a.C, a.ws != nullptr);
+  const DownArgs d = {(const uint8_t*)a.X, a.ldx, a.K, (const uint16_t*)a.down, a.lddown, a.R, a.scale, a.x_scale, a.D, a.ldd};
+  const UpArgs o = {(const uint16_t*)a.up, a.ldup, a.C, (const uint16_t*)a.base, a.ldbase, (uint16_t*)a.out, a.ldout};
+  if (p.both) {
+    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_both<DT, RP / 16>), dim3((unsigned)(slots(a.seg, 16) * p.slices)), dim3(512), s, a.seg, d, o, p.slices);
+    return;
   }
-  if (a.C > 0) large ? up<RP, 64>(a, s) : up<RP, 16>(a, s);
+  const dim3 grid((unsigned)(slots(a.seg, p.large ? 64 : 32) * p.splits));
+  if (p.large) SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, 4>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
+  else SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, 2>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
+  const int fblocks = a.C > 0 ? (a.C + 511) / 512 : 1;               // without features D is still to be added up
+  if (a.C > 0 || p.splits > 1)
+    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_up<RP, 2>), dim3((unsigned)(slots(a.seg, 32) * fblocks)), dim3(256), s, a.seg, d, o, fblocks, p.splits, a.ws);
+}
+template <int DT>
+void apply(const AdapterApply& a, hipStream_t s) {
+  switch (padded_rank(a.R)) {
+    case 16: apply<DT, 16>(a, s); break;
+    case 32: apply<DT, 32>(a, s); break;
+    case 64: apply<DT, 64>(a, s); break;
+    default: apply<DT, 128>(a, s); break;
+  }
 }
 
-int outer_chunk(int64_t T, int64_t I, int64_t O) {
-  // about 1024 workgroups of 128 features, whole rounds of 128 rows
-  const int64_t blocks = (I + 127) / 128 + (O + 127) / 128;
-  int64_t chunk = T * blocks / 1024 / 128 * 128;
-  if (chunk < 128) chunk = 128;
-  if (chunk > 1 << 20) chunk = 1 << 20;
-  return (int)chunk;
-}
-
-template <int MT>
-void outer(const AdapterSegments& g, int R, const AdapterOuter& a, int chunk, float* part, hipStream_t s) {
-  const int fblocks = (a.C + 127) / 128;
-  const dim3 grid((unsigned)(slots(g, chunk) * fblocks));
-#define OUTER(RT) \
-  SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_outer<MT, RT>), grid, dim3(256), s, g, a.L, a.ldl, R, (const uint8_t*)a.M, a.ldm, a.blocks, a.ldblocks, a.C, fblocks, chunk, part)
-  switch (padded_rank(R)) {
-    case 16: OUTER(1); break;
-    case 32: OUTER(2); break;
-    case 64: OUTER(4); break;
-    default: OUTER(8); break;
-  }
-#undef OUTER
+// Rows of a chunk of the weight gradients: about 384 workgroups of 512 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 43 us;
+// 512 workgroups 50, 768 47, 1024 55).  A chunk's sum has R / rows times four of its rows' bytes, written and read again: where that gives fewer than 4 R
+// rows (rank 64, 7777 rows of 1280 + 5120: 51 us; 8 R 62), 4 R unless that leaves fewer than 256 workgroups.
+int outer_chunk(int64_t T, int R, int64_t I, int64_t O) {
+  const int64_t blocks = ((I + 511) / 512 + (O + 511) / 512) * (R > 64 ? 2 : 1), least = 4 * padded_rank(R), most = 1 << 20;
+  const auto rows = [&](int64_t workgroups) { return (T * blocks / workgroups + 63) / 64 * 64; };
+  int64_t chunk = rows(384);
+  if (chunk < least) chunk = rows(256) < least ? rows(256) : least;
+  return (int)(chunk < 64 ? 64 : chunk > most ? most : chunk);
 }
 
 }  // namespace
 
 hipError_t launch_adapter_apply(const AdapterApply& a, hipStream_t s) {
   if (a.seg.T == 0) return hipSuccess;
-  switch (padded_rank(a.R)) {
-    case 16: apply<16>(a, s); break;
-    case 32: apply<32>(a, s); break;
-    case 64: apply<64>(a, s); break;
-    default: apply<128>(a, s); break;
+  switch (mode(a.dtype)) {
+    case M_BF16: apply<M_BF16>(a, s); break;
+    case M_E4M3: apply<M_E4M3>(a, s); break;
+    default: apply<M_E5M2>(a, s); break;
   }
   return hipGetLastError();
+}
+
+size_t adapter_apply_workspace_bytes(int64_t T, int segments, int R, int64_t K, int64_t C) {
+  const AdapterSegments g = {nullptr, nullptr, segments, 0, (int)T};
+  if (T == 0) return 0;
+  const ApplyPlan p = plan_apply(g, R, (int)K, (int)C, true);
+  return p.both || p.splits == 1 ? 0 : (size_t)p.splits * (size_t)T * (size_t)R * 4;
 }
 
 size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, int64_t O) {
   if (T == 0) return 0;
   const AdapterSegments g = {nullptr, nullptr, segments, 0, (int)T};
-  return (size_t)slots(g, outer_chunk(T, I, O)) * (size_t)R * (size_t)(I + O) * 4;
+  return (size_t)slots(g, outer_chunk(T, R, I, O)) * (size_t)R * (size_t)(I + O) * 4;
 }
 
 hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOuter& a, const AdapterOuter& b, int accumulate, void* ws, hipStream_t s) {
-  const int chunk = outer_chunk(g.T, a.C, b.C);
-  float* part[2] = {(float*)ws, (float*)ws + slots(g, chunk) * R * a.C};
-  const AdapterOuter* both[2] = {&a, &b};
-  if (g.T > 0)
-    for (int k = 0; k < 2; k++) {
-      if (both[k]->C == 0) continue;
-      switch (mode(both[k]->m_dtype)) {
-        case M_BF16: outer<M_BF16>(g, R, *both[k], chunk, part[k], s); break;
-        case M_E4M3: outer<M_E4M3>(g, R, *both[k], chunk, part[k], s); break;
-        case M_E5M2: outer<M_E5M2>(g, R, *both[k], chunk, part[k], s); break;
-        default: outer<M_BLOCK>(g, R, *both[k], chunk, part[k], s); break;
-      }
+  const int chunk = outer_chunk(g.T, R, a.C, b.C);
+  const auto args = [&](const AdapterOuter& o, float* part) {
+    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + 511) / 512, part};
+  };
+  const OuterArgs x = args(a, (float*)ws), z = args(b, (float*)ws + slots(g, chunk) * R * a.C);
+  if (g.T > 0 && x.fblocks + z.fblocks > 0) {
+    const int64_t n = slots(g, chunk) * (x.fblocks + z.fblocks);
+    const dim3 grid((unsigned)(R > 64 ? (n + 7) / 8 * 16 : n));
+    switch (padded_rank(R)) {
+      case 16: SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer<1>, grid, dim3(256), s, g, x, z, R, chunk); break;
+      case 32: SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer<2>, grid, dim3(256), s, g, x, z, R, chunk); break;
+      default: SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer<4>, grid, dim3(256), s, g, x, z, R, chunk); break;
     }
+  }
   const int ablocks = (a.C + 1023) / 1024, bblocks = (b.C + 1023) / 1024;
   if (ablocks + bblocks > 0 && g.adapters > 0)
     SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_sum, dim3((unsigned)(ablocks + bblocks), (unsigned)R, (unsigned)g.adapters), dim3(256), s, g, R, chunk,
-                (OuterSum{part[0], a.G, a.ldg, a.m_scale, a.C}), (OuterSum{part[1], b.G, b.ldg, b.m_scale, b.C}), ablocks, accumulate);
+                (OuterSum{x.part, a.G, a.ldg, a.m_scale, a.C}), (OuterSum{z.part, b.G, b.ldg, b.m_scale, b.C}), ablocks, accumulate);
   return hipGetLastError();
 }
 

@@ -17,6 +17,7 @@ static int check_matrix(const char* who, const char* name, const void* p, int64_
   if (rows == 0 || cols == 0) return SSTE_OK;            // never addressed
   if (ld % step != 0 || !aligned(p, 16)) return fail(SSTE_ERR_ALIGN, "%s: %s must be 16-byte aligned with a leading dimension that is a multiple of %d", who, name, step);
   if (!p) return fail(SSTE_ERR_NULL, "%s: NULL %s", who, name);
+  if (ld > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: leading dimension of %s above 2^23", who, name);
   if (product_reaches(rows, ld, 1ll << 40)) return fail(SSTE_ERR_UNSUPPORTED, "%s: %s has more than 2^40 elements", who, name);
   return SSTE_OK;
 }
@@ -36,7 +37,7 @@ static int check_segments(const char* who, int64_t T, const int32_t* row_start, 
 static int check_width(const char* who, const char* name, int64_t n, int dtype) {
   const int step = is_8bit(dtype) ? 16 : 8;
   if (n < 0) return fail(SSTE_ERR_SHAPE, "%s: negative size", who);
-  if (n % step != 0 || n > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: %s=%lld must be a multiple of %d up to 2^24", who, name, (long long)n, step);
+  if (n % step != 0 || n > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: %s=%lld must be a multiple of %d up to 2^23", who, name, (long long)n, step);
   return SSTE_OK;
 }
 
@@ -48,7 +49,7 @@ static int check_width(const char* who, const char* name, int64_t n, int dtype) 
 
 // D = scale_n x_scale X down_n^T and out = base + D up_n; K and C: widths of X and out, named as the caller knows them
 static int apply(const char* who, const char* xname, const char* dname, const char* oname, const char* kname, const char* cname, const char* down_name, const char* up_name,
-                 bool e5m2, AdapterApply a, int64_t T, int64_t segments, int64_t adapters, int64_t R, int64_t K, int64_t C, hipStream_t s) {
+                 bool e5m2, void* ws, size_t ws_bytes, AdapterApply a, int64_t T, int64_t segments, int64_t adapters, int64_t R, int64_t K, int64_t C, hipStream_t s) {
   TRY(check_segments(who, T, a.seg.row_start, segments, a.seg.adapter, adapters, R));
   if (a.dtype != SSTE_BF16 && a.dtype != SSTE_F8E4M3 && !(e5m2 && a.dtype == SSTE_F8E5M2)) return fail(SSTE_ERR_DTYPE, "%s: dtype %d", who, a.dtype);
   if (!good_scale(a.x_scale) || (a.dtype == SSTE_BF16 && a.x_scale != 1.0f)) return fail(SSTE_ERR_VALUE, "%s: the scale of %s must be finite and > 0, and 1 for bf16", who, xname);
@@ -63,6 +64,9 @@ static int apply(const char* who, const char* xname, const char* dname, const ch
   if (a.base == a.out && a.base && T > 1 && a.ldbase != a.ldout) return fail(SSTE_ERR_VALUE, "%s: base may be %s itself only with the same leading dimension", who, oname);
   if (!aligned(a.scale, 4)) return fail(SSTE_ERR_ALIGN, "%s: scale must be 4-byte aligned", who);
   if (product_reaches(T / 16 + segments + 2, (C + 511) / 512, 1ll << 31)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  // without the workspace (none, too small, misaligned) the contraction is not split: the same function, slower for few rows
+  const size_t need = adapter_apply_workspace_bytes(T, (int)segments, (int)R, K, C);
+  a.ws = ws && ws_bytes >= need && need > 0 && aligned(ws, 16) ? (float*)ws : nullptr;
   a.seg.segments = (int)segments;
   a.seg.adapters = (int)adapters;
   a.seg.T = (int)T;
@@ -81,22 +85,22 @@ extern "C" {
 int sste_adapter_fwd(const void* X, int64_t T, int64_t I, int64_t ldx, int dtype, float x_scale,
                      const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
                      const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t O,
-                     const void* base, int64_t ldbase, void* Z, int64_t ldz, float* S, int64_t lds, void* hip_stream) {
+                     const void* base, int64_t ldbase, void* Z, int64_t ldz, float* S, int64_t lds, void* workspace, size_t workspace_bytes, void* hip_stream) {
   clear_error();
-  AdapterApply a = {{row_start, seg_adapter, 0, 0, 0}, X, ldx, dtype, x_scale, A, lda, B, ldb, scale, 0, 0, 0, base, ldbase, Z, ldz, S, lds};
-  return apply("adapter_fwd", "X", "S", "Z", "I", "O", "A", "B", false, a, T, segments, adapters, R, I, O, (hipStream_t)hip_stream);
+  AdapterApply a = {{row_start, seg_adapter, 0, 0, 0}, X, ldx, dtype, x_scale, A, lda, B, ldb, scale, 0, 0, 0, base, ldbase, Z, ldz, S, lds, nullptr};
+  return apply("adapter_fwd", "X", "S", "Z", "I", "O", "A", "B", false, workspace, workspace_bytes, a, T, segments, adapters, R, I, O, (hipStream_t)hip_stream);
 }
 
 int sste_adapter_dgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
                        const int32_t* row_start, int64_t segments, const int32_t* seg_adapter,
                        const void* A, int64_t lda, const void* B, int64_t ldb, const float* scale, int64_t adapters, int64_t R, int64_t I,
-                       const void* base, int64_t ldbase, void* dX, int64_t lddx, float* dS, int64_t ldds, void* hip_stream) {
+                       const void* base, int64_t ldbase, void* dX, int64_t lddx, float* dS, int64_t ldds, void* workspace, size_t workspace_bytes, void* hip_stream) {
   clear_error();
-  AdapterApply a = {{row_start, seg_adapter, 0, 0, 0}, dZ, lddz, dtype, dz_scale, B, ldb, A, lda, scale, 0, 0, 0, base, ldbase, dX, lddx, dS, ldds};
-  return apply("adapter_dgrad", "dZ", "dS", "dX", "O", "I", "B", "A", true, a, T, segments, adapters, R, O, I, (hipStream_t)hip_stream);
+  AdapterApply a = {{row_start, seg_adapter, 0, 0, 0}, dZ, lddz, dtype, dz_scale, B, ldb, A, lda, scale, 0, 0, 0, base, ldbase, dX, lddx, dS, ldds, nullptr};
+  return apply("adapter_dgrad", "dZ", "dS", "dX", "O", "I", "B", "A", true, workspace, workspace_bytes, a, T, segments, adapters, R, O, I, (hipStream_t)hip_stream);
 }
 
-static int check_wgrad_sizes(const char* who, int64_t T, int64_t segments, int64_t R, int64_t I, int64_t O) {
+static int check_sizes(const char* who, int64_t T, int64_t segments, int64_t R, int64_t I, int64_t O) {
   TRY(check_segments(who, T, nullptr, 0, nullptr, 0, R));
   if (segments < 0) return fail(SSTE_ERR_SHAPE, "%s: negative number of segments", who);
   if (segments > kAdapterMaxSegments) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^20 segments", who);
@@ -105,9 +109,15 @@ static int check_wgrad_sizes(const char* who, int64_t T, int64_t segments, int64
   return SSTE_OK;
 }
 
+size_t sste_adapter_workspace_bytes(int64_t T, int64_t segments, int64_t R, int64_t in, int64_t out) {
+  clear_error();
+  if (check_sizes("adapter_workspace_bytes", T, segments, R, in, out) != SSTE_OK) return 0;
+  return adapter_apply_workspace_bytes(T, (int)segments, (int)R, in, out);
+}
+
 size_t sste_adapter_wgrad_workspace_bytes(int64_t T, int64_t segments, int64_t R, int64_t I, int64_t O) {
   clear_error();
-  if (check_wgrad_sizes("adapter_wgrad_workspace_bytes", T, segments, R, I, O) != SSTE_OK) return 0;
+  if (check_sizes("adapter_wgrad_workspace_bytes", T, segments, R, I, O) != SSTE_OK) return 0;
   return adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
 }
 
@@ -131,8 +141,8 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
   TRY(check_matrix(who, "X", X, T, I, ldx, is_8bit(x_dtype) ? 16 : 8));
   if (x_dtype == SSTE_F8BLOCK) {
     if (ldxb < (I + 31) / 32) return fail(SSTE_ERR_SHAPE, "%s: ldxb smaller than the blocks of a row", who);
+    if (ldxb > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: ldxb above 2^23", who);
     if (T > 0 && I > 0 && !x_blocks) return fail(SSTE_ERR_NULL, "%s: a checkpoint of X needs its scales", who);
-    if (product_reaches(T, ldxb, 1ll << 40)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^40 scales", who);
   } else {
     x_blocks = nullptr;
     ldxb = 0;
@@ -141,7 +151,7 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
   TRY(check_matrix(who, "dS", dS, T, R, ldds, 4));
   TRY(check_matrix(who, "dA", dA, adapters * R, I, ldda, 4));
   TRY(check_matrix(who, "dB", dB, adapters * R, O, lddb, 4));
-  if (product_reaches(T / 128 + segments + 2, (I > O ? I : O) / 128 + 1, 1ll << 31)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  if (product_reaches(T / 64 + segments + 2, I / 512 + O / 512 + 2, 1ll << 31)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
   const size_t need = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SSTE_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, need);
@@ -154,7 +164,7 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
 
 static int check_checkpoint(const char* who, int64_t R, int64_t C, const void* codes, int64_t ldc, const void* scales, int64_t lds) {
   if (R < 0 || C < 0) return fail(SSTE_ERR_SHAPE, "%s: negative size", who);
-  if (C % 16 != 0 || C > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: C=%lld must be a multiple of 16 up to 2^24", who, (long long)C);
+  if (C % 16 != 0 || C > kAdapterMaxWidth) return fail(SSTE_ERR_UNSUPPORTED, "%s: C=%lld must be a multiple of 16 up to 2^23", who, (long long)C);
   if (R >= 1ll << 31) return fail(SSTE_ERR_UNSUPPORTED, "%s: 2^31 rows or more", who);
   TRY(check_matrix(who, "codes", codes, R, C, ldc, 16));
   if (lds < (C + 31) / 32) return fail(SSTE_ERR_SHAPE, "%s: lds smaller than the blocks of a row", who);

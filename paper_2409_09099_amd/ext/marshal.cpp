@@ -25,7 +25,8 @@ namespace {
 struct Entry {                     // one marshalled function: its Python definition (called when the fast path declines)
   PyObject* python = nullptr;
 };
-enum Fn { PROJECT_PACK, SGD_PROJECT_PACK, LINEAR_FWD, LINEAR_FWD_EX, LINEAR_FWD_ACT, LINEAR_DGRAD, LINEAR_DGRAD_ACT, LINEAR_WGRAD, CAST_FP8, N_FN };
+enum Fn { PROJECT_PACK, SGD_PROJECT_PACK, LINEAR_FWD, LINEAR_FWD_EX, LINEAR_FWD_ACT, LINEAR_DGRAD, LINEAR_DGRAD_ACT, LINEAR_WGRAD, CAST_FP8,
+          ADAPTER_FWD, ADAPTER_DGRAD, ADAPTER_WGRAD, CHECKPOINT_PACK, CHECKPOINT_BACKWARD, N_FN };
 Entry g_fn[N_FN];
 PyObject* g_error = nullptr;       // SsteError
 bool g_bound = false;
@@ -40,6 +41,13 @@ decltype(&sste_wgrad_workspace_bytes) p_wgrad_workspace_bytes;
 decltype(&sste_cast_fp8) p_cast_fp8;
 decltype(&sste_project_pack_batch) p_project_pack_batch;
 decltype(&sste_sgd_project_pack_batch) p_sgd_project_pack_batch;
+decltype(&sste_adapter_fwd) p_adapter_fwd;
+decltype(&sste_adapter_dgrad) p_adapter_dgrad;
+decltype(&sste_adapter_wgrad) p_adapter_wgrad;
+decltype(&sste_adapter_workspace_bytes) p_adapter_workspace_bytes;
+decltype(&sste_adapter_wgrad_workspace_bytes) p_adapter_wgrad_workspace_bytes;
+decltype(&sste_checkpoint_pack) p_checkpoint_pack;
+decltype(&sste_checkpoint_backward) p_checkpoint_backward;
 decltype(&sste_last_error) p_last_error;
 
 // ---- arguments ------------------------------------------------------------------------------------------
@@ -124,8 +132,40 @@ Matrix matrix(Args& a, const at::Tensor* t, int itemsize) {
   m.p = t->numel() > 0 ? t->data_ptr() : nullptr;
   return m;
 }
+// matrices one below the other: (adapters, rank, width)
+struct Stack {
+  void* p = nullptr;
+  int64_t n = 0, rank = 0, width = 0, ld = 0;
+};
+Stack stack(Args& a, const at::Tensor* t, int itemsize) {
+  Stack m;
+  if (!a.ok || !t) return m;
+  if (t->dim() != 3 || !t->is_cuda() || (int)t->element_size() != itemsize || (t->size(2) > 1 && t->stride(2) != 1)) return a.ok = false, m;
+  m.n = t->size(0);
+  m.rank = t->size(1);
+  m.width = t->size(2);
+  m.ld = m.n >= 1 && m.rank >= 1 ? std::max(m.width, t->stride(1)) : m.width;
+  if (m.n > 1 && t->stride(0) != m.rank * m.ld) a.ok = false;
+  m.p = t->numel() > 0 ? t->data_ptr() : nullptr;
+  return m;
+}
+// number of segments of a batch's rows
+int64_t segments(Args& a, const at::Tensor* row_start, const at::Tensor* seg_adapter) {
+  if (!a.ok) return 0;
+  for (const at::Tensor* t : {row_start, seg_adapter})
+    if (t->dim() != 1 || t->scalar_type() != at::kInt || !t->is_cuda() || !t->is_contiguous()) return a.ok = false, 0;
+  if (row_start->size(0) != seg_adapter->size(0) + 1) a.ok = false;
+  return seg_adapter->size(0);
+}
+// a matrix of known shape and type; without one, the caller's function declines
+Matrix exactly(Args& a, const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType type) {
+  if (!a.ok || !t) return Matrix();
+  const Matrix m = matrix(a, t, (int)at::elementSize(type));
+  if (t->scalar_type() != type || m.rows != rows || m.cols != cols) a.ok = false;
+  return m;
+}
 void* address(const at::Tensor* t) { return t && t->numel() > 0 ? t->data_ptr() : nullptr; }
-int item(int dtype) { return dtype == SSTE_F8E4M3 || dtype == SSTE_F8E5M2 ? 1 : 2; }
+int item(int dtype) { return dtype == SSTE_F8E4M3 || dtype == SSTE_F8E5M2 || dtype == SSTE_F8BLOCK ? 1 : 2; }
 void* stream_of(const at::Tensor& t) { return (void*)c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 at::Tensor make(const at::Tensor& like, int64_t rows, int64_t cols, at::ScalarType type) {
   return at::empty({rows, cols}, at::TensorOptions().dtype(type).device(like.device()));
@@ -348,6 +388,155 @@ PyObject* cast_fp8(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject*
   return PyTuple_Pack(2, o[3], o[4]);
 }
 
+// the forward pass of the adapters, and their input gradient: X and Z of one are dZ and dX of the other, with A and B exchanged
+PyObject* adapter(Fn f, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames, PyObject* (&o)[12]) {
+  Args a;
+  const at::Tensor *X = a.needed(o[0]), *rs = a.needed(o[1]), *sa = a.needed(o[2]), *A = a.needed(o[3]), *B = a.needed(o[4]), *scale = a.tensor(o[5]), *base = a.tensor(o[6]),
+                   *Z = a.tensor(o[9]), *S = a.tensor(o[10]), *ws = a.tensor(o[11]);
+  const int dt = a.small(o[7], SSTE_BF16);
+  const double xs = a.number(o[8], 1.0);
+  const Matrix x = matrix(a, X, item(dt));
+  const int64_t n_seg = segments(a, rs, sa);
+  const Stack ma = stack(a, A, 2), mb = stack(a, B, 2);
+  if (!a.ok || ma.n != mb.n || ma.rank != mb.rank || (f == ADAPTER_FWD ? ma : mb).width != x.cols) return decline(f, args, nargs, kwnames);
+  if (scale && (scale->dim() != 1 || scale->size(0) != ma.n || scale->scalar_type() != at::kFloat || !scale->is_cuda() || !scale->is_contiguous())) return decline(f, args, nargs, kwnames);
+  const int64_t C = (f == ADAPTER_FWD ? mb : ma).width;
+  const Matrix b = exactly(a, base, x.rows, C, at::kBFloat16);
+  at::Tensor made_z, made_s;
+  if (a.ok && !Z) made_z = make(*X, x.rows, C, at::kBFloat16);
+  if (a.ok && !S) made_s = make(*X, x.rows, ma.rank, at::kFloat);
+  const Matrix z = exactly(a, Z ? Z : &made_z, x.rows, C, at::kBFloat16), sm = exactly(a, S ? S : &made_s, x.rows, ma.rank, at::kFloat);
+  if (!a.ok) return decline(f, args, nargs, kwnames);
+  at::Tensor scratch;
+  if (!ws) {
+    const size_t need = p_adapter_workspace_bytes(x.rows, n_seg, ma.rank, x.cols, C);
+    if (need > 0) {
+      scratch = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(X->device()));
+      ws = &scratch;
+    }
+  }
+  const size_t ws_bytes = ws ? (size_t)ws->numel() * ws->element_size() : 0;
+  void* s = stream_of(*X);
+  const auto call = f == ADAPTER_FWD ? p_adapter_fwd : p_adapter_dgrad;
+  CALL(st, call(x.p, x.rows, x.cols, x.ld, dt, (float)xs, (const int32_t*)address(rs), n_seg, (const int32_t*)address(sa), ma.p, ma.ld, mb.p, mb.ld, (const float*)address(scale), ma.n,
+                ma.rank, C, b.p, b.ld, z.p, z.ld, (float*)sm.p, sm.ld, address(ws), ws_bytes, s));
+  if (st) return fail(st);
+  PyObject *rz = result(o[9], made_z), *rsm = result(o[10], made_s);
+  PyObject* r = rz && rsm ? PyTuple_Pack(2, rz, rsm) : nullptr;
+  Py_XDECREF(rz);
+  Py_XDECREF(rsm);
+  return r;
+}
+PyObject* n_afwd[12];
+PyObject* adapter_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  PyObject* o[12];  // X row_start seg_adapter A B scale base dtype x_scale Z S workspace
+  if (!g_bound || !collect(n_afwd, args, nargs, kwnames, o)) return decline(ADAPTER_FWD, args, nargs, kwnames);
+  return adapter(ADAPTER_FWD, args, nargs, kwnames, o);
+}
+PyObject* n_adgrad[12];
+PyObject* adapter_dgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  PyObject* o[12];  // dZ row_start seg_adapter A B scale base dtype dy_scale dX dS workspace
+  if (!g_bound || !collect(n_adgrad, args, nargs, kwnames, o)) return decline(ADAPTER_DGRAD, args, nargs, kwnames);
+  return adapter(ADAPTER_DGRAD, args, nargs, kwnames, o);
+}
+
+PyObject* n_awgrad[16];
+PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  PyObject* o[16];  // dZ X S dS row_start seg_adapter adapters dtype dy_scale x_dtype x_scale x_blocks dA dB accumulate workspace
+  Args a;
+  if (!g_bound || !collect(n_awgrad, args, nargs, kwnames, o)) return decline(ADAPTER_WGRAD, args, nargs, kwnames);
+  const at::Tensor *dZ = a.needed(o[0]), *X = a.needed(o[1]), *S = a.needed(o[2]), *dS = a.needed(o[3]), *rs = a.needed(o[4]), *sa = a.needed(o[5]), *xb = a.tensor(o[11]), *dA = a.tensor(o[12]),
+                   *dB = a.tensor(o[13]), *ws = a.tensor(o[15]);
+  if (!o[6]) a.ok = false;
+  const int64_t n = a.integer(o[6], 0);
+  const int dt = a.small(o[7], SSTE_BF16), xdt = a.small(o[9], SSTE_BF16);
+  const double dys = a.number(o[8], 1.0), xs = a.number(o[10], 1.0);
+  const int acc = !o[14] || o[14] == Py_False ? 0 : 1;
+  if (o[14] && o[14] != Py_True && o[14] != Py_False) a.ok = false;
+  const Matrix y = matrix(a, dZ, item(dt)), x = matrix(a, X, item(xdt));
+  const int64_t n_seg = segments(a, rs, sa);
+  if (!a.ok || S->dim() != 2 || y.rows != x.rows || n < 0 || (acc && !(dA && dB))) return decline(ADAPTER_WGRAD, args, nargs, kwnames);
+  const int64_t R = S->size(1);
+  const Matrix s0 = exactly(a, S, x.rows, R, at::kFloat), s1 = exactly(a, dS, x.rows, R, at::kFloat);
+  Matrix blocks;
+  if (xdt == SSTE_F8BLOCK) {
+    if (!xb) a.ok = false;
+    blocks = exactly(a, xb, x.rows, (x.cols + 31) / 32, at::kByte);
+  }
+  if (!a.ok) return decline(ADAPTER_WGRAD, args, nargs, kwnames);
+  at::Tensor made_a, made_b, scratch;
+  const auto f32 = at::TensorOptions().dtype(at::kFloat).device(X->device());
+  if (!dA) made_a = at::empty({n, R, x.cols}, f32), dA = &made_a;
+  if (!dB) made_b = at::empty({n, R, y.cols}, f32), dB = &made_b;
+  const Stack ga = stack(a, dA, 4), gb = stack(a, dB, 4);
+  if (!a.ok || dA->scalar_type() != at::kFloat || dB->scalar_type() != at::kFloat || ga.n != n || gb.n != n || ga.rank != R || gb.rank != R || ga.width != x.cols || gb.width != y.cols)
+    return decline(ADAPTER_WGRAD, args, nargs, kwnames);
+  if (!ws) {
+    scratch = at::empty({(int64_t)p_adapter_wgrad_workspace_bytes(x.rows, n_seg, R, x.cols, y.cols)}, at::TensorOptions().dtype(at::kByte).device(X->device()));
+    ws = &scratch;
+  }
+  const size_t ws_bytes = (size_t)ws->numel() * ws->element_size();
+  void* s = stream_of(*X);
+  CALL(st, p_adapter_wgrad(y.p, y.rows, y.cols, y.ld, dt, (float)dys, x.p, x.cols, x.ld, xdt, (float)xs, blocks.p, blocks.ld, (const float*)s0.p, s0.ld, (const float*)s1.p, s1.ld,
+                           (const int32_t*)address(rs), n_seg, (const int32_t*)address(sa), n, R, (float*)ga.p, ga.ld, (float*)gb.p, gb.ld, acc, address(ws), ws_bytes, s));
+  if (st) return fail(st);
+  PyObject *ra = result(o[12], made_a), *rb = result(o[13], made_b);
+  PyObject* r = ra && rb ? PyTuple_Pack(2, ra, rb) : nullptr;
+  Py_XDECREF(ra);
+  Py_XDECREF(rb);
+  return r;
+}
+
+PyObject* n_pack8[3];
+PyObject* checkpoint_pack(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  PyObject* o[3];  // X codes scales
+  Args a;
+  if (!g_bound || !collect(n_pack8, args, nargs, kwnames, o)) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
+  const at::Tensor *X = a.needed(o[0]), *codes = a.tensor(o[1]), *scales = a.tensor(o[2]);
+  const Matrix x = matrix(a, X, 2);
+  if (!a.ok) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
+  const int64_t blocks = (x.cols + 31) / 32;
+  at::Tensor made_c, made_s;
+  if (!codes) made_c = make(*X, x.rows, x.cols, at::kByte);
+  if (!scales) made_s = make(*X, x.rows, blocks, at::kByte);
+  const Matrix c = exactly(a, codes ? codes : &made_c, x.rows, x.cols, at::kByte), b = exactly(a, scales ? scales : &made_s, x.rows, blocks, at::kByte);
+  if (!a.ok) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
+  void* s = stream_of(*X);
+  CALL(st, p_checkpoint_pack(x.p, x.rows, x.cols, x.ld, c.p, c.ld, b.p, b.ld, s));
+  if (st) return fail(st);
+  PyObject *rc = result(o[1], made_c), *rb = result(o[2], made_s);
+  PyObject* r = rc && rb ? PyTuple_Pack(2, rc, rb) : nullptr;
+  Py_XDECREF(rc);
+  Py_XDECREF(rb);
+  return r;
+}
+
+PyObject* n_back8[7];
+PyObject* checkpoint_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  PyObject* o[7];  // codes scales dA act A dH restore
+  Args a;
+  if (!g_bound || !collect(n_back8, args, nargs, kwnames, o)) return decline(CHECKPOINT_BACKWARD, args, nargs, kwnames);
+  const at::Tensor *codes = a.needed(o[0]), *scales = a.needed(o[1]), *dA = a.tensor(o[2]), *A = a.tensor(o[4]), *dH = a.tensor(o[5]);
+  const int act = a.small(o[3], SSTE_ACT_GELU_TANH);
+  const bool restore = !o[6] || o[6] == Py_True;
+  if ((o[6] && o[6] != Py_True && o[6] != Py_False) || (!restore && A) || (!dA && dH)) a.ok = false;
+  const Matrix c = matrix(a, codes, 1), b = exactly(a, scales, c.rows, (c.cols + 31) / 32, at::kByte), d = exactly(a, dA, c.rows, c.cols, at::kBFloat16);
+  if (!a.ok) return decline(CHECKPOINT_BACKWARD, args, nargs, kwnames);
+  at::Tensor made_a, made_h;
+  if (restore && !A) made_a = make(*codes, c.rows, c.cols, at::kBFloat16), A = &made_a;
+  if (dA && !dH) made_h = make(*codes, c.rows, c.cols, at::kBFloat16), dH = &made_h;
+  const Matrix am = exactly(a, A, c.rows, c.cols, at::kBFloat16), h = exactly(a, dH, c.rows, c.cols, at::kBFloat16);
+  if (!a.ok) return decline(CHECKPOINT_BACKWARD, args, nargs, kwnames);
+  void* s = stream_of(*codes);
+  CALL(st, p_checkpoint_backward(c.p, b.p, c.rows, c.cols, c.ld, b.ld, act, am.p, am.ld, d.p, d.ld, h.p, h.ld, s));
+  if (st) return fail(st);
+  PyObject *ra = A ? result(o[4], made_a) : keep(nullptr), *rh = dH ? result(o[5], made_h) : keep(nullptr);
+  PyObject* r = ra && rh ? PyTuple_Pack(2, ra, rh) : nullptr;
+  Py_XDECREF(ra);
+  Py_XDECREF(rh);
+  return r;
+}
+
 // launches of the prepared multi-tensor tables: (table tensor, n_items, total_blocks, val_dtype) and (..., w_dtype, val_dtype, alpha)
 PyObject* pack_batch_launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   Args a;
@@ -386,7 +575,8 @@ bool take(PyObject* d, const char* name, F& f) {
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *addr, *fns, *err;
   if (!PyArg_ParseTuple(args, "O!O!O", &PyDict_Type, &addr, &PyDict_Type, &fns, &err)) return nullptr;
-  const char* const names[N_FN] = {"project_pack", "sgd_project_pack", "linear_fwd", "linear_fwd_ex", "linear_fwd_act", "linear_dgrad", "linear_dgrad_act", "linear_wgrad", "cast_fp8"};
+  const char* const names[N_FN] = {"project_pack", "sgd_project_pack", "linear_fwd", "linear_fwd_ex", "linear_fwd_act", "linear_dgrad", "linear_dgrad_act", "linear_wgrad", "cast_fp8",
+                                  "adapter_fwd", "adapter_dgrad", "adapter_wgrad", "checkpoint_pack", "checkpoint_backward"};
   for (int i = 0; i < N_FN; i++) {
     PyObject* f = PyDict_GetItemString(fns, names[i]);
     if (!f) return PyErr_Format(PyExc_KeyError, "%s", names[i]);
@@ -401,7 +591,9 @@ PyObject* bind(PyObject*, PyObject* args) {
           take(addr, "sste_linear_dgrad_act", p_linear_dgrad_act) && take(addr, "sste_linear_wgrad_at", p_linear_wgrad_at) &&
           take(addr, "sste_wgrad_workspace_bytes", p_wgrad_workspace_bytes) && take(addr, "sste_cast_fp8", p_cast_fp8) &&
           take(addr, "sste_project_pack_batch", p_project_pack_batch) && take(addr, "sste_sgd_project_pack_batch", p_sgd_project_pack_batch) &&
-          take(addr, "sste_last_error", p_last_error)))
+          take(addr, "sste_adapter_fwd", p_adapter_fwd) && take(addr, "sste_adapter_dgrad", p_adapter_dgrad) && take(addr, "sste_adapter_wgrad", p_adapter_wgrad) &&
+          take(addr, "sste_adapter_workspace_bytes", p_adapter_workspace_bytes) && take(addr, "sste_adapter_wgrad_workspace_bytes", p_adapter_wgrad_workspace_bytes) && take(addr, "sste_checkpoint_pack", p_checkpoint_pack) &&
+          take(addr, "sste_checkpoint_backward", p_checkpoint_backward) && take(addr, "sste_last_error", p_last_error)))
       return nullptr;
     g_bound = true;
   }
@@ -429,7 +621,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 PyObject* document(PyObject*, PyObject* docs);
 PyMethodDef methods[] = {
   FAST(project_pack), FAST(sgd_project_pack), FAST(linear_fwd), FAST(linear_fwd_ex), FAST(linear_fwd_act), FAST(linear_dgrad), FAST(linear_dgrad_act),
-  FAST(linear_wgrad), FAST(cast_fp8),
+  FAST(linear_wgrad), FAST(cast_fp8), FAST(adapter_fwd), FAST(adapter_dgrad), FAST(adapter_wgrad), FAST(checkpoint_pack), FAST(checkpoint_backward),
   {"pack_batch_launch", (PyCFunction)(void (*)(void))(PlainCall)guarded<pack_batch_launch>, METH_FASTCALL, "Launches a prepared sste_project_pack_batch table."},
   {"update_batch_launch", (PyCFunction)(void (*)(void))(PlainCall)guarded<update_batch_launch>, METH_FASTCALL, "Launches a prepared sste_sgd_project_pack_batch table."},
   {"bind", bind, METH_VARARGS, "bind(addresses, functions, error)"},
@@ -464,5 +656,10 @@ PyMODINIT_FUNC PyInit__marshal() {
   intern(n_dgrad_act, {"dY", "vals", "meta", "I", "H", "dtype", "dy_scale", "w_scale", "act", "dX"});
   intern(n_wgrad, {"dY", "X", "seed", "offset", "dtype", "dy_scale", "x_scale", "dW", "accumulate", "workspace", "first_token"});
   intern(n_cast, {"X", "scale", "out_dtype", "Q", "amax_out", "store"});
+  intern(n_afwd, {"X", "row_start", "seg_adapter", "A", "B", "scale", "base", "dtype", "x_scale", "Z", "S", "workspace"});
+  intern(n_adgrad, {"dZ", "row_start", "seg_adapter", "A", "B", "scale", "base", "dtype", "dy_scale", "dX", "dS", "workspace"});
+  intern(n_awgrad, {"dZ", "X", "S", "dS", "row_start", "seg_adapter", "adapters", "dtype", "dy_scale", "x_dtype", "x_scale", "x_blocks", "dA", "dB", "accumulate", "workspace"});
+  intern(n_pack8, {"X", "codes", "scales"});
+  intern(n_back8, {"codes", "scales", "dA", "act", "A", "dH", "restore"});
   return PyModule_Create(&module);
 }

@@ -24,6 +24,7 @@ void clear_error() { message[0] = 0; }
 }
 hipError_t launch_adapter_apply(const AdapterApply&, hipStream_t) { reached("adapter_apply"); }
 hipError_t launch_adapter_wgrad(const AdapterSegments&, int, const AdapterOuter&, const AdapterOuter&, int, void*, hipStream_t) { reached("adapter_wgrad"); }
+size_t adapter_apply_workspace_bytes(int64_t T, int, int R, int64_t, int64_t) { return (size_t)T * (size_t)R * 16; }
 size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, int64_t O) { return (size_t)(T / 128 + segments + 2) * (size_t)R * (size_t)(I + O) * 4; }
 hipError_t launch_checkpoint_pack(const void*, int64_t, int64_t, int64_t, void*, int64_t, void*, int64_t, hipStream_t) { reached("checkpoint_pack"); }
 hipError_t launch_checkpoint_backward(const void*, const void*, int64_t, int64_t, int64_t, int64_t, int, void*, int64_t, const void*, int64_t, void*, int64_t, hipStream_t) {
@@ -45,9 +46,9 @@ int main() {
   void* fake = reinterpret_cast<void*>(0x1000);
   float* f = reinterpret_cast<float*>(0x1000);
   const int32_t* seg = reinterpret_cast<const int32_t*>(0x1000);
-  const int64_t huge = INT64_MAX / 2, wide = 1ll << 24, most = (1ll << 30) - 1;
+  const int64_t huge = INT64_MAX / 2, wide = 1ll << 23, most = (1ll << 30) - 1;
   auto fwd = [&](int64_t T, int64_t I, int64_t ldx, int64_t segments, int64_t lda, int64_t adapters, int64_t R, int64_t O, int64_t ldz) {
-    return sste_adapter_fwd(fake, T, I, ldx, SSTE_BF16, 1.f, seg, segments, seg, fake, lda, fake, O, f, adapters, R, O, fake, ldz, fake, ldz, f, R, nullptr);
+    return sste_adapter_fwd(fake, T, I, ldx, SSTE_BF16, 1.f, seg, segments, seg, fake, lda, fake, O, f, adapters, R, O, fake, ldz, fake, ldz, f, R, nullptr, 0, nullptr);
   };
   EXPECT(fwd(huge, 64, 64, 1, 64, 1, 8, 64, 64), SSTE_ERR_UNSUPPORTED);
   EXPECT(fwd(4, huge - huge % 8, huge - huge % 8, 1, huge - huge % 8, 1, 8, 64, 64), SSTE_ERR_UNSUPPORTED);
@@ -69,6 +70,7 @@ int main() {
   EXPECT(wgrad(4, 64, 64, 1, 1, 8, huge - huge % 4, 1 << 20), SSTE_ERR_UNSUPPORTED);
   EXPECT(wgrad(1024, 64, 64, 1, 1, 8, 64, 16), SSTE_ERR_WORKSPACE);
   if (sste_adapter_wgrad_workspace_bytes(huge, huge, huge, huge, huge) != 0) failures++;
+  if (sste_adapter_workspace_bytes(huge, 1, 8, 64, 64) != 0 || sste_adapter_workspace_bytes(4, 1, 8, huge, 64) != 0) failures++;
   (void)sste_adapter_wgrad_workspace_bytes(most, 1 << 20, 128, wide, wide);                   // a number of bytes, whatever it is
   EXPECT(sste_checkpoint_pack(fake, huge, 64, 64, fake, 64, fake, 2, nullptr), SSTE_ERR_UNSUPPORTED);
   EXPECT(sste_checkpoint_pack(fake, 4, huge - huge % 16, huge - huge % 16, fake, huge - huge % 16, fake, huge, nullptr), SSTE_ERR_UNSUPPORTED);

@@ -21,8 +21,8 @@ def err(lib):
 
 
 # argument numbers: 0 X 1 T 2 I 3 ldx 4 dtype 5 x_scale 6 row_start 7 segments 8 seg_adapter 9 A 10 lda 11 B 12 ldb 13 scale 14 adapters 15 R 16 O 17 base 18 ldbase 19 Z 20 ldz
-# 21 S 22 lds 23 stream
-FWD = [FAKE, 4, 64, 64, 0, 1.0, FAKE, 2, FAKE, FAKE, 64, FAKE, 80, FAKE, 3, 16, 80, FAKE, 80, P(0x2000), 80, FAKE, 16, None]
+# 21 S 22 lds 23 workspace 24 bytes 25 stream
+FWD = [FAKE, 4, 64, 64, 0, 1.0, FAKE, 2, FAKE, FAKE, 64, FAKE, 80, FAKE, 3, 16, 80, FAKE, 80, P(0x2000), 80, FAKE, 16, None, 0, None]
 
 
 @pytest.mark.parametrize("change,status", [
@@ -43,7 +43,7 @@ def test_adapter_fwd_refuses(lib, change, status):
 
 
 # 0 dZ 1 T 2 O 3 lddz 4 dtype 5 dz_scale ... 16 I: the same places, A as wide as dX and B as wide as dZ
-DGRAD = [FAKE, 4, 80, 80, 3, 0.5, FAKE, 2, FAKE, FAKE, 64, FAKE, 80, FAKE, 3, 16, 64, FAKE, 64, P(0x2000), 64, FAKE, 16, None]
+DGRAD = [FAKE, 4, 80, 80, 3, 0.5, FAKE, 2, FAKE, FAKE, 64, FAKE, 80, FAKE, 3, 16, 64, FAKE, 64, P(0x2000), 64, FAKE, 16, None, 0, None]
 
 
 @pytest.mark.parametrize("change,status", [({4: 2}, 4), ({4: 4}, 4), ({4: 0}, 5), ({12: 72}, 2), ({10: 56}, 2), ({2: 72, 12: 72}, 7), ({15: 9}, 7), ({20: 56}, 2), ({9: None}, 1), ({11: None}, 1)])
@@ -79,6 +79,19 @@ def test_wgrad_workspace(lib):
     args = list(WGRAD)
     args[28] = sste.adapter_wgrad_workspace_bytes(4, 2, 16, 64, 80) - 1
     assert lib.sste_adapter_wgrad(*args) == 6
+
+
+def test_plans_of_every_size(lib):
+    """The planning of a call is host arithmetic: every combination of ends must come to a size, with nothing divided by zero on the way."""
+    for T in (0, 1, 9, 15, 16, 17, 600, 5000, 9000, 40000, (1 << 30) - 1):
+        for segments in (0, 1, 2, 700, 1 << 20):
+            for R in (8, 16, 32, 64, 128):
+                for a in (0, 8, 64, 5120, 1 << 23):
+                    for b in (0, 8, 1280, 1 << 23):
+                        need = lib.sste_adapter_workspace_bytes(T, segments, R, a, b)
+                        assert (need == 0) if T == 0 else need % (T * R * 4) == 0 and need // (T * R * 4) in (0, 2, 3, 4), (T, segments, R, a, b)
+                        need = lib.sste_adapter_wgrad_workspace_bytes(T, segments, R, a, b)
+                        assert (need == 0) == (T == 0 or a + b == 0) and (a + b == 0 or need % (R * (a + b) * 4) == 0)
 
 
 @pytest.mark.parametrize("change,status", [({1: -1}, 2), ({2: -16}, 2), ({2: 24}, 7), ({1: 1 << 31}, 7), ({3: 32}, 2), ({3: 50}, 3), ({0: ODD}, 3), ({0: None}, 1), ({4: None}, 1), ({6: None}, 1),

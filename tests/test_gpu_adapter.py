@@ -53,9 +53,9 @@ def within(name, got, want, bound):
     assert not bad.any(), (name, int(bad.sum()), np.argwhere(bad)[:4], err[bad][:4], np.broadcast_to(bound, err.shape)[bad][:4])
 
 
-def check_apply(sste, fwd, T, K, C, R, N, starts, ids, kind, base=True, scale=True, in_place=False, pad=0, seed=0, K_std=1.0):
+def check_apply(sste, fwd, T, K, C, R, N, starts, ids, kind, base=True, scale=True, in_place=False, pad=0, seed=0, workspace=None):
     rng = np.random.default_rng(seed)
-    X, x64, dt, xs = stored(sste, normal(rng, (T, K), K_std), kind, pad)
+    X, x64, dt, xs = stored(sste, normal(rng, (T, K), 1.0), kind, pad)
     down = (normal(rng, (N, R, K), 0.05)).to(torch.bfloat16)
     up = (normal(rng, (N, R, C), 0.05)).to(torch.bfloat16)
     s = normal(rng, (N,), 1.0) if scale else None
@@ -65,9 +65,9 @@ def check_apply(sste, fwd, T, K, C, R, N, starts, ids, kind, base=True, scale=Tr
     rows = OA.rows_of(starts, ids, N, T)
     out64, S64, eS, eO = OA.apply(x64, rows, f64(down), f64(up), None if s is None else f64(s), b64)
     if fwd:
-        out, S = sste.adapter_fwd(X, row_start, seg, down, up, scale=s, base=b, dtype=dt, x_scale=xs, Z=b if in_place else None)
+        out, S = sste.adapter_fwd(X, row_start, seg, down, up, scale=s, base=b, dtype=dt, x_scale=xs, Z=b if in_place else None, workspace=workspace)
     else:
-        out, S = sste.adapter_dgrad(X, row_start, seg, up, down, scale=s, base=b, dtype=dt, dy_scale=xs, dX=b if in_place else None)
+        out, S = sste.adapter_dgrad(X, row_start, seg, up, down, scale=s, base=b, dtype=dt, dy_scale=xs, dX=b if in_place else None, workspace=workspace)
     torch.cuda.synchronize()
     within("S", S, S64, eS)
     within("out", out, out64, eO + BF16_STEP * (np.abs(out64) + eO))
@@ -107,10 +107,24 @@ def test_8_bit(sste, T, K, C, R, fwd, kind):
 
 @pytest.mark.parametrize("R", [8, 16, 24, 32, 64, 128])
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
-def test_long_batches(sste, R, kind):
-    """The tiles for many rows, ragged segments among them."""
+@pytest.mark.parametrize("K", [208, 2064])
+def test_long_batches(sste, R, kind, K):
+    """Many rows, in tiles of 32 and (long contractions) of 64, ragged segments among them."""
     T = 8300
-    check_apply(sste, True, T, 208, 264, R, 3, [5, 70, 134, 199, 8200], [2, -1, 0, 1], kind, seed=R)
+    check_apply(sste, True, T, K, 264, R, 3, [5, 70, 134, 199, 8200], [2, -1, 0, 1], kind, seed=R)
+
+
+@pytest.mark.parametrize("R", [8, 32, 64, 128])
+@pytest.mark.parametrize("K", [2056, 5120])
+@pytest.mark.parametrize("fwd", [True, False])
+def test_split_contraction(sste, R, K, fwd):
+    """The first product shared out among workgroups, into a workspace; without one, or with one that is too small, not shared out."""
+    T, C = 700, 136
+    need = sste.adapter_workspace_bytes(T, 3, R, K, C)
+    assert need > 0 and need % (T * R * 4) == 0
+    for workspace in (None, torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(need - 1, dtype=torch.uint8, device="cuda"),
+                      torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")):
+        check_apply(sste, fwd, T, K, C, R, 3, [0, 133, 600, 690], [2, -1, 0], "bf16", workspace=workspace)
 
 
 @pytest.mark.parametrize("base,scale,in_place,pad", [(False, True, False, 0), (True, False, False, 16), (True, True, True, 16), (False, False, False, 0), (True, True, True, 0)])
@@ -285,6 +299,54 @@ def test_same_bits_every_time(sste):
     for _ in range(3):
         again = sste.adapter_wgrad(dZ, X, S, dS, *seg, 2)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_native_marshalling(sste):
+    """The same bits as through the Python definitions, outputs given or made; and the same refusals."""
+    from paper_2409_09099_amd import binding
+    rng = np.random.default_rng(17)
+    T, I, O, R, N = 70, 144, 272, 16, 3
+    X, dZ, A, B = (normal(rng, s, 1).to(torch.bfloat16) for s in ((T, I), (T, O), (N, R, I), (N, R, O)))
+    scale, base = normal(rng, (N,), 1), normal(rng, (T, O), 1).to(torch.bfloat16)
+    seg = segments([0, 30, 70], [2, 0])
+    codes, blocks = sste.checkpoint_pack(X)
+    S = normal(rng, (T, R), 1)
+    X8 = (X.float() / 4).to(torch.float8_e4m3fn)
+    wide = torch.empty((T, O + 8), dtype=torch.bfloat16, device="cuda")
+    calls = [
+        ("adapter_fwd", (X, *seg, A, B), {}), ("adapter_fwd", (X, *seg, A, B, scale, base), dict(Z=wide[:, :O], S=torch.empty_like(S))),
+        ("adapter_fwd", (X8, *seg, A, B), dict(dtype=sste.F8E4M3, x_scale=4)), ("adapter_dgrad", (dZ, *seg, A, B), dict(scale=scale)),
+        ("adapter_wgrad", (dZ, X, S, S, *seg, N), {}), ("adapter_wgrad", (dZ, codes, S, S, *seg, N), dict(x_dtype=sste.F8BLOCK, x_blocks=blocks)),
+        ("adapter_wgrad", (dZ, X, S, S, *seg, N), dict(dA=torch.zeros((N, R, I), device="cuda"), dB=torch.zeros((N, R, O), device="cuda"), accumulate=True)),
+        ("checkpoint_pack", (X,), {}), ("checkpoint_backward", (codes, blocks), {}), ("checkpoint_backward", (codes, blocks, X), dict(act=sste.ACT_NONE, restore=False)),
+        ("checkpoint_backward", (codes, blocks, X), dict(A=torch.empty_like(X), dH=torch.empty_like(X))),
+    ]
+    for name, args, kw in calls:
+        results = []
+        for f in (binding._PYTHON[name], getattr(sste, name)):
+            for k in ("dA", "dB"):
+                if k in kw:
+                    kw[k].fill_(0.5)
+            results.append([None if t is None else t.clone() for t in f(*args, **kw)])
+        assert [t is None for t in results[0]] == [t is None for t in results[1]]
+        assert all(a is None or (a.dtype == b.dtype and torch.equal(a.view(torch.uint8) if a.is_contiguous() else a, b.view(torch.uint8) if b.is_contiguous() else b))
+                   for a, b in zip(*results)), (name, kw.keys())
+    i32 = torch.int32
+    for call in (lambda: sste.adapter_fwd(X, seg[0].long(), seg[1], A, B), lambda: sste.adapter_fwd(X, seg[0], seg[1][:1], A, B), lambda: sste.adapter_fwd(X, *seg, A, B[:2]),
+                 lambda: sste.adapter_fwd(X, *seg, A[:, :8], B), lambda: sste.adapter_fwd(X, *seg, B, A), lambda: sste.adapter_fwd(X, *seg, A, B, scale=scale[:2]),
+                 lambda: sste.adapter_fwd(X, *seg, A, B, base=base[:9]), lambda: sste.adapter_fwd(X, *seg, A, B, Z=base.float()), lambda: sste.adapter_fwd(X, *seg, A, B, S=S[:, :8]),
+                 lambda: sste.adapter_fwd(X, *seg, A.transpose(0, 1).contiguous().transpose(0, 1), B), lambda: sste.adapter_fwd(X.t(), *seg, A, B),
+                 lambda: sste.adapter_dgrad(X, *seg, A, B), lambda: sste.adapter_wgrad(dZ[:9], X, S, S, *seg, N), lambda: sste.adapter_wgrad(dZ, X, S, S[:, :8], *seg, N),
+                 lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, accumulate=True), lambda: sste.adapter_wgrad(dZ, codes, S, S, *seg, N, x_dtype=sste.F8BLOCK),
+                 lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, dA=torch.zeros((N, R, I + 8), device="cuda")),
+                 lambda: sste.checkpoint_pack(X, codes=codes[:9]), lambda: sste.checkpoint_pack(X, scales=torch.empty((T, 4), dtype=i32, device="cuda")),
+                 lambda: sste.checkpoint_backward(codes, blocks[:, :2]), lambda: sste.checkpoint_backward(codes, blocks, dH=X), lambda: sste.checkpoint_backward(codes, blocks, A=X, restore=False)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: sste.adapter_fwd(X, *seg, A[:, :, :], B, dtype=9), lambda: sste.checkpoint_backward(codes, blocks, act=7),
+                 lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(sste.SsteError):
+            call()
 
 
 # ---- together, streams, graphs --------------------------------------------------------------------------------------
