@@ -134,13 +134,19 @@ __device__ __forceinline__ void buffer_store_b128(BufferRsrc r, uint32_t voffset
 // ---- down and up ----------------------------------------------------------------------------------------------
 // Down, for 16 TT rows of one adapter and the contraction's elements k0 .. k1 - 1, by a workgroup of eight waves: KC elements at a time go through LDS,
 // of the rows and of the adapter, loaded in whole pieces of a row (the operands' own layout has a different row in every lane, at a quarter of the load
-// rate) and kept two chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
+// rate) and kept DEPTH chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
 // waves, the waves share the tile's rows and ranks out as well.  The sums of the steps' waves meet in LDS, in the order of the steps.
+// Elements of a chunk: as many as leave room for two or three workgroups a CU; for few rows, where the chunks' latency adds up, twice as many for rank 32 (one
+// row of 1280 -> 3840: 5.7 us against 9.6) and 128 (one row of 1280 -> 1280: 10.5 against 12.1), not for 64 (64 rows of their own 16.1, against 20.8).
+constexpr int down_chunk(int padded_rank, int rows) {
+  return padded_rank == 16 ? 256 : padded_rank == 32 ? (rows == 16 ? 256 : 128) : padded_rank == 64 ? 128 : rows == 16 ? 128 : 64;
+}
 template <int DT, int RT, int TT>
 struct Down {
   static constexpr int RP = RT * 16, TR = TT * 16, EB = DT == M_BF16 ? 2 : 1;
-  static constexpr int KC = RP <= 32 ? 256 : 8192 / RP, STEPS = KC / 32, GROUPS = 8 / STEPS;       // a chunk, its steps, the waves that share a step
+  static constexpr int KC = down_chunk(RP, TR), STEPS = KC / 32, GROUPS = 8 / STEPS;               // a chunk, its steps, the waves that share a step
   static constexpr int GT = GROUPS < TT ? GROUPS : TT, GR = GROUPS / GT, TW = TT / GT, RW = RT / GR;   // shares by rows and by ranks, a wave's own tiles
+  static constexpr int DEPTH = 2;                                                                  // chunks ahead in registers, even
   static constexpr int LDK = KC + 8, LD = RP + 4;                                                  // LDS rows start four banks apart
   static constexpr int PC = KC / 8, XP = (TR * PC + 511) / 512, WP = (RP * PC + 511) / 512;        // pieces of eight elements: of a row, a thread's
   static constexpr int STAGE = (TR + RP) * LDK * 2, RED = STEPS * TR * LD * 4, LDS = 2 * STAGE > RED ? 2 * STAGE : RED;
@@ -202,18 +208,18 @@ struct Down {
         for (int j = 0; j < TW; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(w), frag(x[j]), acc[i][j], 0, 0, 0);
       }
     };
-    Chunk a, b;
-    load(a, k0);
-    load(b, k0 + KC);
-    for (int k = k0; k < k1; k += 2 * KC) {            // a chunk behind k1 is zeros
-      put(a, 0);
-      __syncthreads();
-      load(a, k + 2 * KC);
-      multiply(0);
-      put(b, 1);                                       // the barrier before it is behind the last reads of this buffer
-      __syncthreads();
-      load(b, k + 3 * KC);
-      multiply(1);
+    Chunk c[DEPTH];
+#pragma unroll
+    for (int i = 0; i < DEPTH; i++) load(c[i], k0 + i * KC);
+    for (int k = k0; k < k1; k += DEPTH * KC) {
+#pragma unroll
+      for (int i = 0; i < DEPTH; i++) {
+        if (k + i * KC >= k1) break;
+        put(c[i], i & 1);                              // the barrier before is behind the last reads of this buffer
+        __syncthreads();
+        load(c[i], k + (DEPTH + i) * KC);
+        multiply(i & 1);
+      }
     }
     __syncthreads();
     // lane (m, q) holds ranks 4 q .. 4 q + 3 of row m
@@ -662,11 +668,11 @@ struct ApplyPlan {
   bool large;        // two launches: tiles of 64 rows for the first, otherwise of 32
   int splits, span;  // of its contraction
 };
-int apply_chunk(int R) { return padded_rank(R) <= 32 ? 256 : 8192 / padded_rank(R); }      // Down::KC
 ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspace) {
   ApplyPlan p = {};
   const int64_t extra = (g.segments < g.T ? g.segments : g.T) + 1;     // tiles that segments, and the rows outside them, may add
-  const int chunk = apply_chunk(R), chunks = (K + chunk - 1) / chunk;
+  const int rank = padded_rank(R);
+  int chunk = down_chunk(rank, 16), chunks = (K + chunk - 1) / chunk;
   // One launch saves one, about 3 us, and does the first product in 16-row tiles without sharing its contraction out.  Rank 16, 1280 -> 3840: 1 row 5.6
   // against 8.6, 1024 rows 9.2 against 11.2; rank 64, 1280 -> 5120: 512 rows 11.7 against 12.3, 1024 rows 16.7 against 14.9; rank 16, 5120 -> 1280 (20
   // chunks): 64 rows of two segments 8.5 against 9.1, 256 rows of four 11.6 against 9.2, 256 rows of as many 12.7 against 16.5.
@@ -674,16 +680,17 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   p.both = (int64_t)g.T * chunks <= 5120 && (chunks <= 10 || g.T <= 64 || single);
   if (p.both) {
     const int64_t tiles = g.T / 16 + extra, passes = (C + 1023) / 1024;
-    p.slices = (int)(1024 / tiles < passes ? 1024 / tiles : passes);
+    p.slices = (int)(520 / tiles < passes ? 520 / tiles : passes);
     if (p.slices < 1) p.slices = 1;
     return p;
   }
   // 64-row tiles read the adapter half as often.  Rank 64, 5120 -> 1280, 16384 rows: 68 against 80, 2999 rows 22.2 against 20.3 (too few tiles); rank 64,
   // 1024 -> 4096, 8192 rows 44.9 against 44.4 (a short contraction gains nothing); rank 16, 4096 -> 1024, 16384 ragged rows 51 against 46 (a small adapter).
-  const bool wide = padded_rank(R) >= 64;
+  const bool wide = rank >= 64;
   p.large = wide && g.T >= 8192 && (K >= 2048 || g.T >= 32768);
   // The contraction is shared out, in whole chunks and at least four of them, until there are about 512 workgroups with many ranks, 1024 with few: rank 64,
   // 2999 ragged rows of 5120: 21.6 in four, 24 in three, 31 in one; rank 16, 16384 ragged rows of 4096: 51 in one, 47 in two, 46 in three.
+  chunk = down_chunk(rank, p.large ? 64 : 32), chunks = (K + chunk - 1) / chunk;
   const int64_t tiles = g.T / (p.large ? 64 : 32) + extra;
   int64_t splits = ((wide ? 512 : 1024) + tiles / 2) / tiles;
   if (splits > chunks / 4) splits = chunks / 4;
