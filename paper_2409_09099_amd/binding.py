@@ -508,6 +508,14 @@ def _given(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, 
     return ld
 
 
+def _together(first: torch.Tensor, *others: Optional[torch.Tensor]) -> "torch.cuda.device":
+    """Refuses tensors of several devices; the context in which `first`'s device is the current one."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors of a call must be on the same device")
+    return torch.cuda.device(first.device)
+
+
 def _bytes(t: Optional[torch.Tensor]) -> int:
     return t.numel() * t.element_size() if t is not None else 0
 
@@ -534,8 +542,10 @@ def adapter_fwd(X: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Ten
     S, lds = _result(S, T, R, torch.float32, X, "S")
     ldbase = _given(base, T, O, torch.bfloat16, "base")
     workspace = _adapter_workspace(workspace, T, segments, R, I, O, X)
-    _check(library().sste_adapter_fwd(_ptr(X), T, I, ldx, dtype, x_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
-                                      _ptr(scale), n, R, O, _ptr(base), ldbase, _ptr(Z), ldz, _ptr(S), lds, _ptr(workspace), _bytes(workspace), _stream(X)))
+    with _together(X, row_start, seg_adapter, A, B, scale, base, Z, S, workspace):
+        _check(library().sste_adapter_fwd(_ptr(X), T, I, ldx, dtype, x_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
+                                          _ptr(scale), n, R, O, _ptr(base), ldbase, _ptr(Z), ldz, _ptr(S), lds, _ptr(workspace), _bytes(workspace),
+                                          _stream(X)))
     return Z, S
 
 
@@ -550,9 +560,10 @@ def adapter_dgrad(dZ: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.
     dS, ldds = _result(dS, T, R, torch.float32, dZ, "dS")
     ldbase = _given(base, T, I, torch.bfloat16, "base")
     workspace = _adapter_workspace(workspace, T, segments, R, O, I, dZ)
-    _check(library().sste_adapter_dgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
-                                        _ptr(scale), n, R, I, _ptr(base), ldbase, _ptr(dX), lddx, _ptr(dS), ldds, _ptr(workspace), _bytes(workspace),
-                                        _stream(dZ)))
+    with _together(dZ, row_start, seg_adapter, A, B, scale, base, dX, dS, workspace):
+        _check(library().sste_adapter_dgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(row_start), segments, _ptr(seg_adapter), _ptr(A), lda, _ptr(B), ldb,
+                                            _ptr(scale), n, R, I, _ptr(base), ldbase, _ptr(dX), lddx, _ptr(dS), ldds, _ptr(workspace), _bytes(workspace),
+                                            _stream(dZ)))
     return dX, dS
 
 
@@ -590,9 +601,10 @@ def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.
         raise ValueError("dA and dB must be float32 tensors (adapters, rank, I) and (adapters, rank, O)")
     if workspace is None:
         workspace = torch.empty(adapter_wgrad_workspace_bytes(T, segments, R, I, O), dtype=torch.uint8, device=X.device)
-    _check(library().sste_adapter_wgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(X), I, ldx, x_dtype, x_scale, _ptr(x_blocks), ldxb, _ptr(S), lds,
-                                        _ptr(dS), ldds, _ptr(row_start), segments, _ptr(seg_adapter), adapters, R, _ptr(dA), ldda, _ptr(dB), lddb,
-                                        int(bool(accumulate)), _ptr(workspace), _bytes(workspace), _stream(X)))
+    with _together(dZ, X, S, dS, row_start, seg_adapter, x_blocks if x_dtype == F8BLOCK else None, dA, dB, workspace):
+        _check(library().sste_adapter_wgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(X), I, ldx, x_dtype, x_scale, _ptr(x_blocks), ldxb, _ptr(S), lds,
+                                            _ptr(dS), ldds, _ptr(row_start), segments, _ptr(seg_adapter), adapters, R, _ptr(dA), ldda, _ptr(dB), lddb,
+                                            int(bool(accumulate)), _ptr(workspace), _bytes(workspace), _stream(X)))
     return dA, dB
 
 
@@ -602,7 +614,8 @@ def checkpoint_pack(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scale
     R, C, ldx = _matrix(X, 2, "X")
     codes, ldc = _result(codes, R, C, torch.uint8, X, "codes")
     scales, lds = _result(scales, R, (C + 31) // 32, torch.uint8, X, "scales")
-    _check(library().sste_checkpoint_pack(_ptr(X), R, C, ldx, _ptr(codes), ldc, _ptr(scales), lds, _stream(X)))
+    with _together(X, codes, scales):
+        _check(library().sste_checkpoint_pack(_ptr(X), R, C, ldx, _ptr(codes), ldc, _ptr(scales), lds, _stream(X)))
     return codes, scales
 
 
@@ -622,8 +635,9 @@ def checkpoint_backward(codes: torch.Tensor, scales: torch.Tensor, dA: Optional[
         dH, lddh = _result(dH, R, C, torch.bfloat16, codes, "dH")
     elif dH is not None:
         raise ValueError("dH needs dA")
-    _check(library().sste_checkpoint_backward(_ptr(codes), _ptr(scales), R, C, ldc, lds, act, _ptr(A), lda, _ptr(dA), ldda, _ptr(dH), lddh,
-                                              _stream(codes)))
+    with _together(codes, scales, A, dA, dH):
+        _check(library().sste_checkpoint_backward(_ptr(codes), _ptr(scales), R, C, ldc, lds, act, _ptr(A), lda, _ptr(dA), ldda, _ptr(dH), lddh,
+                                                  _stream(codes)))
     return A, dH
 
 

@@ -18,9 +18,9 @@ struct AdapterSegments {
   int segments, adapters, T;
 };
 
-// Widest low rank, and its granule; most rows and segments (row numbers and tile numbers fit 32 bits)
+// Widest low rank, and its granule; rows and segments whose tiles a grid can count (2^32 threads); widths whose tiles 32-bit offsets reach
 constexpr int kAdapterMaxRank = 128, kAdapterRankStep = 8;
-constexpr int64_t kAdapterMaxRows = 1ll << 30, kAdapterMaxSegments = 1ll << 20, kAdapterMaxAdapters = 65535, kAdapterMaxWidth = 1ll << 23;
+constexpr int64_t kAdapterMaxRows = 1ll << 27, kAdapterMaxSegments = 1ll << 20, kAdapterMaxAdapters = 65535, kAdapterMaxWidth = 1ll << 23, kAdapterMaxGrid = 1ll << 24;
 
 // D = scale_n x_scale X down_n^T (T x R float32), out = base + D up_n (T x C bf16).  X is T x K of dtype; down_n is R x K, up_n is R x C, stacked.
 struct AdapterApply {

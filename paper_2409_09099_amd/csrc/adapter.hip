@@ -14,6 +14,8 @@ namespace {
 
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // ---- rows to tiles --------------------------------------------------------------------------------------------
 // The grids are sized from T and the number of segments alone; the segments' bounds stay on the device.  With the rows before the first
 // and behind the last segment as two more (without an adapter), bounds b_0 = 0 <= b_1 <= ... <= b_{S+2} = T, segment v's tiles of TR rows
@@ -21,7 +23,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 // Bounds are clamped to 0 .. T, so that no array of bounds leads outside the matrices.
 struct Tile {
   int64_t row;    // first row
-  int rows;       // <= 0: an empty slot
+  int rows;       // 0: an empty slot
   int adapter;    // -1: none
 };
 __device__ __forceinline__ int segment_bound(const AdapterSegments& g, int v) {
@@ -53,9 +55,11 @@ __device__ __forceinline__ Tile find_tile(const AdapterSegments& g, int slot, in
   const uint64_t mask = __ballot(lane < n && (int)((uint32_t)bound / (uint32_t)tr) + v <= slot) | 1;
   const int hit = __builtin_amdgcn_readfirstlane(63 - __clzll((long long)mask));       // at most 62: the next lane has the next bound
   const int b0 = __builtin_amdgcn_readlane(bound, hit), b1 = __builtin_amdgcn_readlane(bound, hit + 1);
+  // (Divisions leave their results in vector registers; as scalars again, or every descriptor made from them costs a loop over the lanes.)
   Tile t;
-  t.row = b0 + (int64_t)(slot - (int)((uint32_t)b0 / (uint32_t)tr) - lo - hit) * tr;
-  t.rows = (int)min((int64_t)tr, b1 - t.row);
+  const int64_t row = b0 + (int64_t)(slot - (int)((uint32_t)b0 / (uint32_t)tr) - lo - hit) * tr;
+  t.row = uniform((int)min(row, (int64_t)g.T));
+  t.rows = uniform((int)max(min((int64_t)tr, b1 - row), (int64_t)0));
   t.adapter = __builtin_amdgcn_readlane(adapter, hit);
   return t;
 }
@@ -134,8 +138,8 @@ __device__ __forceinline__ void buffer_store_b128(BufferRsrc r, uint32_t voffset
 // ---- down and up ----------------------------------------------------------------------------------------------
 // Down, for 16 TT rows of one adapter and the contraction's elements k0 .. k1 - 1, by a workgroup of eight waves: KC elements at a time go through LDS,
 // of the rows and of the adapter, loaded in whole pieces of a row (the operands' own layout has a different row in every lane, at a quarter of the load
-// rate) and kept DEPTH chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
-// waves, the waves share the tile's rows and ranks out as well.  The sums of the steps' waves meet in LDS, in the order of the steps.
+// rate) and kept two chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
+// waves, the waves share the ranks out as well.  The sums of the steps' waves meet in LDS, in the order of the steps.
 // Elements of a chunk: as many as leave room for two or three workgroups a CU; for few rows, where the chunks' latency adds up, twice as many for rank 32 (one
 // row of 1280 -> 3840: 5.7 us against 9.6) and 128 (one row of 1280 -> 1280: 10.5 against 12.1), not for 64 (64 rows of their own 16.1, against 20.8).
 constexpr int down_chunk(int padded_rank, int rows) {
@@ -145,10 +149,10 @@ template <int DT, int RT, int TT>
 struct Down {
   static constexpr int RP = RT * 16, TR = TT * 16, EB = DT == M_BF16 ? 2 : 1;
   static constexpr int KC = down_chunk(RP, TR), STEPS = KC / 32, GROUPS = 8 / STEPS;               // a chunk, its steps, the waves that share a step
-  static constexpr int GT = GROUPS < TT ? GROUPS : TT, GR = GROUPS / GT, TW = TT / GT, RW = RT / GR;   // shares by rows and by ranks, a wave's own tiles
-  static constexpr int DEPTH = 2;                                                                  // chunks ahead in registers, even
+  static constexpr int RW = RT / GROUPS;                                                          // by ranks; every wave has all rows: fewest operands a result
   static constexpr int LDK = KC + 8, LD = RP + 4;                                                  // LDS rows start four banks apart
-  static constexpr int PC = KC / 8, XP = (TR * PC + 511) / 512, WP = (RP * PC + 511) / 512;        // pieces of eight elements: of a row, a thread's
+  static constexpr int PC = KC / 8, XP = (TR * PC + 511) / 512, WP = RP * PC / 512;                // pieces of eight elements: of a row, a thread's
+  static_assert(RP * PC % 512 == 0 && (TR * PC % 512 == 0 || 512 % (TR * PC) == 0), "whole rounds of pieces");
   static constexpr int STAGE = (TR + RP) * LDK * 2, RED = STEPS * TR * LD * 4, LDS = 2 * STAGE > RED ? 2 * STAGE : RED;
   template <bool BITS8> struct Raw { using T = uint4; };
   template <> struct Raw<true> { using T = uint2; };
@@ -157,19 +161,19 @@ struct Down {
   // Leaves the steps' sums in lds as float [STEPS][TR][LD], behind a barrier.
   static __device__ __forceinline__ void run(uint8_t* lds, const Tile& t, const uint8_t* __restrict__ X, int64_t ldx, int K, int k0, int k1, const uint16_t* __restrict__ W, int64_t ldw, int R) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
-    const int step = wave % STEPS, t0 = (wave / STEPS) % GT * TW, r0 = (wave / STEPS) / GT * RW;
-    f32x4 acc[RW][TW];
+    const int step = wave % STEPS, r0 = wave / STEPS * RW;
+    f32x4 acc[RW][TT];
 #pragma unroll
     for (int i = 0; i < RW; i++)
 #pragma unroll
-      for (int j = 0; j < TW; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
+      for (int j = 0; j < TT; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
     // Rows behind the tile's, ranks behind R and elements behind k1 are zeros; nothing is read for them.
     const BufferRsrc rx = make_rsrc(X + t.row * ldx * EB, ((uint32_t)(t.rows - 1) * (uint32_t)ldx + (uint32_t)K) * EB);
     const BufferRsrc rw = rows_of(W, (int64_t)t.adapter * R, R, ldw, K);
     auto load = [&](Chunk& c, int k) {
 #pragma unroll
       for (int i = 0; i < XP; i++) {
-        const int p = i * 512 + tid, r = p / PC, e = k + p % PC * 8;
+        const int p = (i * 512 + tid) % (TR * PC), r = p / PC, e = k + p % PC * 8;      // of fewer pieces than threads some are loaded twice
         const uint32_t at = e < k1 ? ((uint32_t)r * (uint32_t)ldx + (uint32_t)e) * EB : kNowhere;
         if constexpr (DT == M_BF16) c.x[i] = buffer_load_b128(rx, at, 0);
         else c.x[i] = buffer_load_b64(rx, at, 0);
@@ -184,8 +188,7 @@ struct Down {
       uint8_t* to = lds + buffer * STAGE;
 #pragma unroll
       for (int i = 0; i < XP; i++) {
-        const int p = i * 512 + tid, r = p / PC;
-        if (TR * PC % 512 != 0 && r >= TR) continue;
+        const int p = (i * 512 + tid) % (TR * PC), r = p / PC;
         uint4* d = (uint4*)(to + (r * LDK + p % PC * 8) * 2);
         if constexpr (DT == M_BF16) *d = c.x[i];
         else *d = widen<DT>(c.x[i], 1.0f);
@@ -193,33 +196,40 @@ struct Down {
 #pragma unroll
       for (int i = 0; i < WP; i++) {
         const int p = i * 512 + tid, r = p / PC;
-        if (RP * PC % 512 == 0 || r < RP) *(uint4*)(to + ((TR + r) * LDK + p % PC * 8) * 2) = c.w[i];
+        *(uint4*)(to + ((TR + r) * LDK + p % PC * 8) * 2) = c.w[i];
       }
     };
     auto multiply = [&](int buffer) {
       const uint16_t* from = (const uint16_t*)(lds + buffer * STAGE) + step * 32 + q * 8;
-      uint4 x[TW];
+      uint4 x[TT];
 #pragma unroll
-      for (int j = 0; j < TW; j++) x[j] = *(const uint4*)(from + ((t0 + j) * 16 + m) * LDK);
+      for (int j = 0; j < TT; j++) x[j] = *(const uint4*)(from + (j * 16 + m) * LDK);
 #pragma unroll
       for (int i = 0; i < RW; i++) {
         const uint4 w = *(const uint4*)(from + (TR + (r0 + i) * 16 + m) * LDK);
 #pragma unroll
-        for (int j = 0; j < TW; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(w), frag(x[j]), acc[i][j], 0, 0, 0);
+        for (int j = 0; j < TT; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(w), frag(x[j]), acc[i][j], 0, 0, 0);
       }
     };
-    Chunk c[DEPTH];
-#pragma unroll
-    for (int i = 0; i < DEPTH; i++) load(c[i], k0 + i * KC);
-    for (int k = k0; k < k1; k += DEPTH * KC) {
-#pragma unroll
-      for (int i = 0; i < DEPTH; i++) {
-        if (k + i * KC >= k1) break;
-        put(c[i], i & 1);                              // the barrier before is behind the last reads of this buffer
-        __syncthreads();
-        load(c[i], k + (DEPTH + i) * KC);
-        multiply(i & 1);
-      }
+    // (No branches in here: with one, the compiler waits for every load that is under way where it needs the oldest.)
+    Chunk a, b;
+    load(a, k0);
+    load(b, k0 + KC);
+    int k = k0;
+    for (; k + KC < k1; k += 2 * KC) {
+      put(a, 0);
+      __syncthreads();
+      load(a, k + 2 * KC);
+      multiply(0);
+      put(b, 1);                                       // the barrier before is behind the last reads of this buffer
+      __syncthreads();
+      load(b, k + 3 * KC);
+      multiply(1);
+    }
+    if (k < k1) {
+      put(a, 0);
+      __syncthreads();
+      multiply(0);
     }
     __syncthreads();
     // lane (m, q) holds ranks 4 q .. 4 q + 3 of row m
@@ -227,7 +237,7 @@ struct Down {
 #pragma unroll
     for (int i = 0; i < RW; i++)
 #pragma unroll
-      for (int j = 0; j < TW; j++) *(f32x4*)&red[step][(t0 + j) * 16 + m][(r0 + i) * 16 + 4 * q] = acc[i][j];
+      for (int j = 0; j < TT; j++) *(f32x4*)&red[step][j * 16 + m][(r0 + i) * 16 + 4 * q] = acc[i][j];
     __syncthreads();
   }
   // Ranks c .. c + 3 of a row
@@ -372,7 +382,7 @@ k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, int slices) {
   using D = Down<DT, RT, 1>;
   __shared__ __align__(16) uint8_t lds[D::LDS];
   __shared__ __align__(16) Up<RT * 16, 1> up;
-  const int slot = (int)blockIdx.x / slices, slice = (int)blockIdx.x - slot * slices;
+  const int slot = uniform((int)blockIdx.x / slices), slice = (int)blockIdx.x - slot * slices;
   const Tile t = find_tile(g, slot, 16);
   if (t.rows <= 0) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -404,7 +414,7 @@ __global__ void __launch_bounds__(512)
 k_adapter_down(AdapterSegments g, DownArgs d, int splits, int span, float* __restrict__ part) {
   using D = Down<DT, RT, TT>;
   __shared__ __align__(16) uint8_t lds[D::LDS];
-  const int slot = (int)blockIdx.x / splits, split = (int)blockIdx.x - slot * splits;
+  const int slot = uniform((int)blockIdx.x / splits), split = (int)blockIdx.x - slot * splits;
   const Tile t = find_tile(g, slot, TT * 16);
   if (t.rows <= 0) return;
   if (t.adapter < 0) {
@@ -427,7 +437,7 @@ template <int RP, int TT>
 __global__ void __launch_bounds__(256, RP <= 32 ? 3 : 2)
 k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, int fblocks, int splits, const float* __restrict__ part) {
   __shared__ __align__(16) Up<RP, TT> up;
-  const int slot = (int)blockIdx.x / fblocks, fb = (int)blockIdx.x - slot * fblocks;
+  const int slot = uniform((int)blockIdx.x / fblocks), fb = (int)blockIdx.x - slot * fblocks;
   const Tile t = find_tile(g, slot, TT * 16);
   if (t.rows <= 0) return;
   const int f = (fb * 4 + ((int)threadIdx.x >> 6)) * 128;
@@ -500,16 +510,17 @@ struct OuterRows {
   }
   // `f`: the lane's features, or kNowhere
   __device__ __forceinline__ void load(const OuterArgs& a, const Tile& t, int r0, uint32_t f) {
-    const uint32_t q = ((uint32_t)threadIdx.x & 63) >> 4;
+    uint32_t q8 = (((uint32_t)threadIdx.x & 63) >> 4) * 8;
+    asm("" : "+v"(q8));                                // offsets anew in each step: kept, they would take registers that the sums need
     const int rows = min(t.rows - r0, 32);
     const BufferRsrc r = BITS8 ? rows_of(a.M, t.row + r0, rows, a.ldm, a.C) : rows_of((const uint16_t*)a.M, t.row + r0, rows, a.ldm, a.C);
 #pragma unroll
-    for (int i = 0; i < 8; i++) words(x[i], r, f == kNowhere ? f : ((q * 8 + i) * (uint32_t)a.ldm + f) * (BITS8 ? 1 : 2));
+    for (int i = 0; i < 8; i++) words(x[i], r, f == kNowhere ? f : ((q8 + i) * (uint32_t)a.ldm + f) * (BITS8 ? 1 : 2));
     if constexpr (BITS8) {
       const BufferRsrc rs = rows_of(a.type == M_BLOCK ? a.blocks : nullptr, t.row + r0, rows, a.ldblocks, (a.C + 31) / 32);
 #pragma unroll
       for (int i = 0; i < 8; i++)
-        e[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(f == kNowhere ? f : (q * 8 + i) * (uint32_t)a.ldblocks + (f >> 5)), 0, 0);
+        e[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(f == kNowhere ? f : (q8 + i) * (uint32_t)a.ldblocks + (f >> 5)), 0, 0);
     }
   }
   // b[j]: rows 0 .. 7 of feature j
@@ -554,9 +565,11 @@ struct Outer {
 
     float v[8];
     auto load_l = [&](int r0) {
+      uint32_t q8 = (uint32_t)q * 8;
+      asm("" : "+v"(q8));
       const BufferRsrc r = rows_of(a.L, t.row + r0, min(t.rows - r0, 32), a.ldl, R);
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[e] = u2f((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)(fw < RT && mine < R ? ((uint32_t)(q * 8 + e) * (uint32_t)a.ldl + (uint32_t)mine) * 4 : kNowhere), 0, 0));
+      for (int e = 0; e < 8; e++) v[e] = u2f((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)(fw < RT && mine < R ? ((q8 + e) * (uint32_t)a.ldl + (uint32_t)mine) * 4 : kNowhere), 0, 0));
     };
     OuterRows<BITS8> m;
     load_l(0);
@@ -600,7 +613,7 @@ k_adapter_outer(AdapterSegments g, OuterArgs x, OuterArgs z, int R, int chunk) {
   __shared__ __align__(16) uint8_t lds[Outer<RT>::LDS];
   const bool pairs = R > 64;
   const int block = pairs ? (int)blockIdx.x / 16 * 8 + (int)blockIdx.x % 8 : (int)blockIdx.x, rank0 = pairs ? ((int)blockIdx.x / 8 & 1) * 64 : 0;
-  const int fblocks = x.fblocks + z.fblocks, slot = block / fblocks;
+  const int fblocks = x.fblocks + z.fblocks, slot = uniform(block / fblocks);
   if (slot >= g.T / chunk + g.segments + 2) return;                                // the last pairs may be empty
   int fb = block - slot * fblocks;
   const bool second = fb >= x.fblocks;

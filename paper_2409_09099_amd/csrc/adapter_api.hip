@@ -28,7 +28,7 @@ static int check_segments(const char* who, int64_t T, const int32_t* row_start, 
   if (R > kAdapterMaxRank || R % kAdapterRankStep != 0)
     return fail(SSTE_ERR_UNSUPPORTED, "%s: rank %lld is not a multiple of %d up to %d (pad A and B with rows of zeros)", who, (long long)R, kAdapterRankStep, kAdapterMaxRank);
   if (T >= kAdapterMaxRows || segments > kAdapterMaxSegments || adapters > kAdapterMaxAdapters)
-    return fail(SSTE_ERR_UNSUPPORTED, "%s: 2^30 rows or more, more than 2^20 segments or more than 65535 adapters", who);
+    return fail(SSTE_ERR_UNSUPPORTED, "%s: 2^27 rows or more, more than 2^20 segments or more than 65535 adapters", who);
   if (segments > 0 && (!row_start || !seg_adapter)) return fail(SSTE_ERR_NULL, "%s: NULL row_start or seg_adapter", who);
   if (!aligned(row_start, 4) || !aligned(seg_adapter, 4)) return fail(SSTE_ERR_ALIGN, "%s: row_start and seg_adapter must be 4-byte aligned", who);
   return SSTE_OK;
@@ -63,7 +63,7 @@ static int apply(const char* who, const char* xname, const char* dname, const ch
   if (a.base) TRY(check_matrix(who, "base", a.base, T, C, a.ldbase, 8));
   if (a.base == a.out && a.base && T > 1 && a.ldbase != a.ldout) return fail(SSTE_ERR_VALUE, "%s: base may be %s itself only with the same leading dimension", who, oname);
   if (!aligned(a.scale, 4)) return fail(SSTE_ERR_ALIGN, "%s: scale must be 4-byte aligned", who);
-  if (product_reaches(T / 16 + segments + 2, (C + 511) / 512, 1ll << 31)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  if (product_reaches(T / 32 + segments + 2, (C + 511) / 512, kAdapterMaxGrid)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
   // without the workspace (none, too small, misaligned) the contraction is not split: the same function, slower for few rows
   const size_t need = adapter_apply_workspace_bytes(T, (int)segments, (int)R, K, C);
   a.ws = ws && ws_bytes >= need && need > 0 && aligned(ws, 16) ? (float*)ws : nullptr;
@@ -151,7 +151,7 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
   TRY(check_matrix(who, "dS", dS, T, R, ldds, 4));
   TRY(check_matrix(who, "dA", dA, adapters * R, I, ldda, 4));
   TRY(check_matrix(who, "dB", dB, adapters * R, O, lddb, 4));
-  if (product_reaches(T / 64 + segments + 2, I / 512 + O / 512 + 2, 1ll << 31)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  if (product_reaches(T / 64 + segments + 2, 2 * (I / 512 + O / 512 + 2), kAdapterMaxGrid)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
   const size_t need = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SSTE_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, need);

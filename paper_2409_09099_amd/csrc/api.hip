@@ -74,7 +74,7 @@ using namespace sste;
 
 extern "C" {
 
-int sste_version(void) { return 100; }
+int sste_version(void) { return 200; }
 
 int sste_timing_begin(int max_launches) {
   clear_error();

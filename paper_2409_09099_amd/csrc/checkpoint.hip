@@ -13,24 +13,24 @@ namespace {
 
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 
-// A lane converts pieces of 16 consecutive elements, two neighbouring lanes share a block of 32.  A workgroup takes whole rows, U pieces a
+// A lane converts pieces of 16 consecutive elements, two neighbouring lanes share a block of 32.  A workgroup takes groups of whole rows, U pieces a
 // thread; a row counts an even number of pieces, the last of them empty where the row ends in the middle of a block.
 struct Rows {
   int64_t rows;
   int per_row;          // pieces of a row, even
   int columns;          // its elements, a multiple of 16
-  int group;            // rows of a workgroup
-  uint32_t magic;       // i / per_row = mulhi(i, magic) for the piece numbers of a workgroup; 0 where a workgroup has one row
+  int group;            // rows of a group
+  uint32_t magic;       // i / per_row = mulhi(i, magic) for the piece numbers of a group; 0 where a group is one row
 };
 struct Piece {
   int64_t row;
   int at;               // piece of the row
   bool in;              // holds elements
 };
-__device__ __forceinline__ Piece piece(const Rows& g, int i) {
+__device__ __forceinline__ Piece piece(const Rows& g, int64_t first, int i) {
   const int r = (int)__umulhi((uint32_t)i, g.magic);
   Piece p;
-  p.row = (int64_t)blockIdx.x * g.group + r;
+  p.row = first + r;
   p.at = i - r * g.per_row;
   p.in = i < g.group * g.per_row && p.row < g.rows && p.at * 16 < g.columns;
   return p;
@@ -50,12 +50,13 @@ __device__ __forceinline__ float scaled(uint32_t bits, float s) { return (bits &
 template <int U>
 __global__ void __launch_bounds__(256)
 k_checkpoint_pack(Rows g, const uint8_t* __restrict__ X, int64_t ldx, uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scales, int64_t lds) {
+  for (int64_t row0 = (int64_t)blockIdx.x * g.group; row0 < g.rows; row0 += (int64_t)gridDim.x * g.group)
   for (int i0 = 0; i0 < g.group * g.per_row; i0 += 256 * U) {
     uint4 x[U][2];
     Piece p[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      p[u] = piece(g, i0 + u * 256 + threadIdx.x);
+      p[u] = piece(g, row0, i0 + u * 256 + threadIdx.x);
       const uint4* s = (const uint4*)(X + (p[u].row * ldx + p[u].at * 16) * 2);
       x[u][0] = load16(s, p[u].in);
       x[u][1] = load16(s + 1, p[u].in);
@@ -86,13 +87,14 @@ template <bool GELU, bool ACT, bool GRAD, int U>
 __global__ void __launch_bounds__(256)
 k_checkpoint_backward(Rows g, const uint8_t* __restrict__ codes, int64_t ldc, const uint8_t* __restrict__ scales, int64_t lds, uint8_t* A, int64_t lda,
                       const uint8_t* dA, int64_t ldda, uint8_t* dH, int64_t lddh) {
+  for (int64_t row0 = (int64_t)blockIdx.x * g.group; row0 < g.rows; row0 += (int64_t)gridDim.x * g.group)
   for (int i0 = 0; i0 < g.group * g.per_row; i0 += 256 * U) {
     uint4 c[U], d[U][2];
     float s[U];
     Piece p[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      p[u] = piece(g, i0 + u * 256 + threadIdx.x);
+      p[u] = piece(g, row0, i0 + u * 256 + threadIdx.x);
       c[u] = load16(codes + p[u].row * ldc + p[u].at * 16, p[u].in);
       s[u] = 1.0f;
       if (p[u].in) s[u] = u2f((uint32_t)scales[p[u].row * lds + (p[u].at >> 1)] << 23);
@@ -138,14 +140,18 @@ Rows rows_of(int64_t R, int64_t C, int pieces) {
   g.magic = g.group == 1 ? 0 : (uint32_t)(((1ull << 32) + g.per_row - 1) / g.per_row);
   return g;
 }
-unsigned groups(const Rows& g) { return (unsigned)((g.rows + g.group - 1) / g.group); }
+// A workgroup a group of rows, as far as a grid can count
+unsigned workgroups(const Rows& g) {
+  const int64_t n = (g.rows + g.group - 1) / g.group;
+  return (unsigned)(n < (1 << 22) ? n : 1 << 22);
+}
 
 }  // namespace
 
 hipError_t launch_checkpoint_pack(const void* X, int64_t R, int64_t C, int64_t ldx, void* codes, int64_t ldc, void* scales, int64_t lds, hipStream_t s) {
   if (R == 0 || C == 0) return hipSuccess;
   const Rows g = rows_of(R, C, 512);
-  SSTE_LAUNCH(SSTE_K_CHECKPOINT, k_checkpoint_pack<2>, dim3(groups(g)), dim3(256), s, g, (const uint8_t*)X, ldx, (uint8_t*)codes, ldc, (uint8_t*)scales, lds);
+  SSTE_LAUNCH(SSTE_K_CHECKPOINT, k_checkpoint_pack<2>, dim3(workgroups(g)), dim3(256), s, g, (const uint8_t*)X, ldx, (uint8_t*)codes, ldc, (uint8_t*)scales, lds);
   return hipGetLastError();
 }
 
@@ -154,7 +160,7 @@ hipError_t launch_checkpoint_backward(const void* codes, const void* scales, int
   if (R == 0 || C == 0) return hipSuccess;
   const Rows g = rows_of(R, C, 512);
 #define BACKWARD(GELU, ACT, GRAD)                                                                                                                        \
-  SSTE_LAUNCH(SSTE_K_CHECKPOINT, (k_checkpoint_backward<GELU, ACT, GRAD, 2>), dim3(groups(g)), dim3(256), s, g, (const uint8_t*)codes, ldc,             \
+  SSTE_LAUNCH(SSTE_K_CHECKPOINT, (k_checkpoint_backward<GELU, ACT, GRAD, 2>), dim3(workgroups(g)), dim3(256), s, g, (const uint8_t*)codes, ldc,             \
               (const uint8_t*)scales, lds, (uint8_t*)A, lda, (const uint8_t*)dA, ldda, (uint8_t*)dH, lddh)
   const bool gelu = act == SSTE_ACT_GELU_TANH;
   if (A && dH) { if (gelu) BACKWARD(true, true, true); else BACKWARD(false, true, true); }

@@ -11,12 +11,14 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/sste.h"
 
@@ -156,6 +158,12 @@ int64_t segments(Args& a, const at::Tensor* row_start, const at::Tensor* seg_ada
     if (t->dim() != 1 || t->scalar_type() != at::kInt || !t->is_cuda() || !t->is_contiguous()) return a.ok = false, 0;
   if (row_start->size(0) != seg_adapter->size(0) + 1) a.ok = false;
   return seg_adapter->size(0);
+}
+// all on the device of the first
+void together(Args& a, const at::Tensor* first, std::initializer_list<const at::Tensor*> others) {
+  if (!a.ok) return;
+  for (const at::Tensor* t : others)
+    if (t && t->device() != first->device()) a.ok = false;
 }
 // a matrix of known shape and type; without one, the caller's function declines
 Matrix exactly(Args& a, const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType type) {
@@ -405,6 +413,7 @@ PyObject* adapter(Fn f, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnam
   at::Tensor made_z, made_s;
   if (a.ok && !Z) made_z = make(*X, x.rows, C, at::kBFloat16);
   if (a.ok && !S) made_s = make(*X, x.rows, ma.rank, at::kFloat);
+  together(a, X, {rs, sa, A, B, scale, base, Z, S, ws});
   const Matrix z = exactly(a, Z ? Z : &made_z, x.rows, C, at::kBFloat16), sm = exactly(a, S ? S : &made_s, x.rows, ma.rank, at::kFloat);
   if (!a.ok) return decline(f, args, nargs, kwnames);
   at::Tensor scratch;
@@ -416,6 +425,7 @@ PyObject* adapter(Fn f, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnam
     }
   }
   const size_t ws_bytes = ws ? (size_t)ws->numel() * ws->element_size() : 0;
+  const c10::DeviceGuard guard(X->device());
   void* s = stream_of(*X);
   const auto call = f == ADAPTER_FWD ? p_adapter_fwd : p_adapter_dgrad;
   CALL(st, call(x.p, x.rows, x.cols, x.ld, dt, (float)xs, (const int32_t*)address(rs), n_seg, (const int32_t*)address(sa), ma.p, ma.ld, mb.p, mb.ld, (const float*)address(scale), ma.n,
@@ -469,6 +479,7 @@ PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
   if (!dA) made_a = at::empty({n, R, x.cols}, f32), dA = &made_a;
   if (!dB) made_b = at::empty({n, R, y.cols}, f32), dB = &made_b;
   const Stack ga = stack(a, dA, 4), gb = stack(a, dB, 4);
+  together(a, dZ, {X, S, dS, rs, sa, xdt == SSTE_F8BLOCK ? xb : nullptr, dA, dB, ws});
   if (!a.ok || dA->scalar_type() != at::kFloat || dB->scalar_type() != at::kFloat || ga.n != n || gb.n != n || ga.rank != R || gb.rank != R || ga.width != x.cols || gb.width != y.cols)
     return decline(ADAPTER_WGRAD, args, nargs, kwnames);
   if (!ws) {
@@ -476,6 +487,7 @@ PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
     ws = &scratch;
   }
   const size_t ws_bytes = (size_t)ws->numel() * ws->element_size();
+  const c10::DeviceGuard guard(X->device());
   void* s = stream_of(*X);
   CALL(st, p_adapter_wgrad(y.p, y.rows, y.cols, y.ld, dt, (float)dys, x.p, x.cols, x.ld, xdt, (float)xs, blocks.p, blocks.ld, (const float*)s0.p, s0.ld, (const float*)s1.p, s1.ld,
                            (const int32_t*)address(rs), n_seg, (const int32_t*)address(sa), n, R, (float*)ga.p, ga.ld, (float*)gb.p, gb.ld, acc, address(ws), ws_bytes, s));
@@ -500,7 +512,9 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
   if (!codes) made_c = make(*X, x.rows, x.cols, at::kByte);
   if (!scales) made_s = make(*X, x.rows, blocks, at::kByte);
   const Matrix c = exactly(a, codes ? codes : &made_c, x.rows, x.cols, at::kByte), b = exactly(a, scales ? scales : &made_s, x.rows, blocks, at::kByte);
+  together(a, X, {codes, scales});
   if (!a.ok) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
+  const c10::DeviceGuard guard(X->device());
   void* s = stream_of(*X);
   CALL(st, p_checkpoint_pack(x.p, x.rows, x.cols, x.ld, c.p, c.ld, b.p, b.ld, s));
   if (st) return fail(st);
@@ -526,7 +540,9 @@ PyObject* checkpoint_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs
   if (restore && !A) made_a = make(*codes, c.rows, c.cols, at::kBFloat16), A = &made_a;
   if (dA && !dH) made_h = make(*codes, c.rows, c.cols, at::kBFloat16), dH = &made_h;
   const Matrix am = exactly(a, A, c.rows, c.cols, at::kBFloat16), h = exactly(a, dH, c.rows, c.cols, at::kBFloat16);
+  together(a, codes, {scales, A, dA, dH});
   if (!a.ok) return decline(CHECKPOINT_BACKWARD, args, nargs, kwnames);
+  const c10::DeviceGuard guard(codes->device());
   void* s = stream_of(*codes);
   CALL(st, p_checkpoint_backward(c.p, b.p, c.rows, c.cols, c.ld, b.ld, act, am.p, am.ld, d.p, d.ld, h.p, h.ld, s));
   if (st) return fail(st);

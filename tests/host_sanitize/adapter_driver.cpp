@@ -46,7 +46,7 @@ int main() {
   void* fake = reinterpret_cast<void*>(0x1000);
   float* f = reinterpret_cast<float*>(0x1000);
   const int32_t* seg = reinterpret_cast<const int32_t*>(0x1000);
-  const int64_t huge = INT64_MAX / 2, wide = 1ll << 23, most = (1ll << 30) - 1;
+  const int64_t huge = INT64_MAX / 2, wide = 1ll << 23, most = (1ll << 27) - 1;
   auto fwd = [&](int64_t T, int64_t I, int64_t ldx, int64_t segments, int64_t lda, int64_t adapters, int64_t R, int64_t O, int64_t ldz) {
     return sste_adapter_fwd(fake, T, I, ldx, SSTE_BF16, 1.f, seg, segments, seg, fake, lda, fake, O, f, adapters, R, O, fake, ldz, fake, ldz, f, R, nullptr, 0, nullptr);
   };
@@ -59,7 +59,7 @@ int main() {
   EXPECT(fwd(4, 64, 64, 1, 64, 1, 8, huge - huge % 8, huge - huge % 8), SSTE_ERR_UNSUPPORTED);
   EXPECT(fwd(most, wide, wide, 1, wide, 65535, 128, wide, wide), SSTE_ERR_UNSUPPORTED);      // more than 2^40 elements
   EXPECT(fwd(64, wide, wide, 1 << 20, huge - huge % 8, 65535, 128, wide, wide), SSTE_ERR_UNSUPPORTED);
-  EXPECT(fwd(1 << 16, 8, 8, 1 << 20, 8, 1, 8, wide, wide), SSTE_ERR_UNSUPPORTED);             // more than 2^31 tiles
+  EXPECT(fwd(1 << 16, 8, 8, 1 << 20, 8, 1, 8, wide, wide), SSTE_ERR_UNSUPPORTED);             // more than 2^24 tiles
   EXPECT(fwd(INT64_MIN, 64, 64, 1, 64, 1, 8, 64, 64), SSTE_ERR_SHAPE);
   auto wgrad = [&](int64_t T, int64_t I, int64_t O, int64_t segments, int64_t adapters, int64_t R, int64_t ldda, size_t bytes) {
     return sste_adapter_wgrad(fake, T, O, O, SSTE_BF16, 1.f, fake, I, I, SSTE_BF16, 1.f, nullptr, 0, f, R, f, R, seg, segments, seg, adapters, R, f, ldda, f, O, 0, fake, bytes, nullptr);
