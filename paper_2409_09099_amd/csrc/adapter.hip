@@ -28,7 +28,7 @@ struct Tile {
 };
 __device__ __forceinline__ int segment_bound(const AdapterSegments& g, int v) {
   if (v <= 0) return 0;
-  if (v >= g.segments + 2) return g.T;
+  if (v >= g.segments + 2 || g.segments == 0) return g.T;              // without segments there may be no arrays
   return min(max(g.row_start[v - 1], 0), g.T);
 }
 __device__ __forceinline__ int first_slot(const AdapterSegments& g, int v, int tr) { return (int)((uint32_t)segment_bound(g, v) / (uint32_t)tr) + v; }

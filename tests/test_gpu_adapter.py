@@ -56,8 +56,7 @@ def within(name, got, want, bound):
 def check_apply(sste, fwd, T, K, C, R, N, starts, ids, kind, base=True, scale=True, in_place=False, pad=0, seed=0, workspace=None):
     rng = np.random.default_rng(seed)
     X, x64, dt, xs = stored(sste, normal(rng, (T, K), 1.0), kind, pad)
-    down = (normal(rng, (N, R, K), 0.05)).to(torch.bfloat16)
-    up = (normal(rng, (N, R, C), 0.05)).to(torch.bfloat16)
+    down, up = (torch.full((N, R, w + pad), float("nan"), dtype=torch.bfloat16, device="cuda")[:, :, :w].copy_(normal(rng, (N, R, w), 0.05)) for w in (K, C))
     s = normal(rng, (N,), 1.0) if scale else None
     b = stored(sste, normal(rng, (T, C), 1.0), "bf16", pad)[0] if base else None
     b64 = None if b is None else f64(b)
@@ -163,6 +162,21 @@ def test_empty(sste, T):
     within("S", S, want[1], want[2])
 
 
+@pytest.mark.parametrize("T", [5, 8200])
+def test_no_segments_need_no_arrays(sste, T):
+    """segments = 0 through the C ABI, with NULL for both arrays."""
+    rng = np.random.default_rng(4)
+    X, base = normal(rng, (T, 64), 1).to(torch.bfloat16), normal(rng, (T, 72), 1).to(torch.bfloat16)
+    A, B = normal(rng, (2, 8, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 72), 1).to(torch.bfloat16)
+    Z, S = torch.full_like(base, 7), torch.full((T, 8), 7.0, device="cuda")
+    dA, dB = torch.full((2, 8, 64), 7.0, device="cuda"), torch.full((2, 8, 72), 7.0, device="cuda")
+    ws = torch.empty(sste.adapter_wgrad_workspace_bytes(T, 0, 8, 64, 72), dtype=torch.uint8, device="cuda")
+    lib, p, stream = sste.library(), lambda t: t.data_ptr(), torch.cuda.current_stream().cuda_stream      # noqa: E731
+    assert lib.sste_adapter_fwd(p(X), T, 64, 64, 0, 1.0, None, 0, None, p(A), 64, p(B), 72, None, 2, 8, 72, p(base), 72, p(Z), 72, p(S), 8, None, 0, stream) == 0
+    assert lib.sste_adapter_wgrad(p(base), T, 72, 72, 0, 1.0, p(X), 64, 64, 0, 1.0, None, 0, p(S), 8, p(S), 8, None, 0, None, 2, 8, p(dA), 64, p(dB), 72, 0, p(ws), ws.numel(), stream) == 0
+    assert torch.equal(Z, base) and not S.any() and not dA.any() and not dB.any()
+
+
 @pytest.mark.parametrize("T", [40, 8200])
 def test_malformed_segments_stay_inside(sste, T):
     """Bounds beyond the rows are clamped, and bounds that decrease leave the memory around the outputs alone."""
@@ -177,6 +191,10 @@ def test_malformed_segments_stay_inside(sste, T):
         torch.cuda.synchronize()
         for room, w in ((room_z, 72), (room_s, 8)):
             assert (room[:16] == 7).all() and (room[-16:] == 7).all() and (room[:, w:] == 7).all()
+        need = sste.adapter_wgrad_workspace_bytes(T, len(ids), 8, 64, 72)
+        ws, room_g = torch.full((need + 256,), 0x11, dtype=torch.uint8, device="cuda"), torch.full((4, 8, 64), 7.0, device="cuda")
+        sste.adapter_wgrad(Z, X, S, S, rs, sa, 2, dA=room_g[1:3], workspace=ws[:need])
+        assert (ws[need:] == 0x11).all() and (room_g[0] == 7).all() and (room_g[3] == 7).all()
     rs, sa = segments([-5, 20, T + 100], [0, 1])
     got, want = sste.adapter_fwd(X, rs, sa, A, B), sste.adapter_fwd(X, *segments([0, 20, T], [0, 1]), A, B)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
