@@ -530,7 +530,8 @@ int sste_cast_fp8(const void* X, int64_t R, int64_t C, int64_t ldx, int out_dtyp
  *   R            in  a multiple of 8 up to 128
  *   dtype        in  of X: SSTE_BF16 (x_scale 1) or SSTE_F8E4M3; of dZ also SSTE_F8E5M2.  I and O: multiples of 8, of 16 where they are the width
  *                    of an 8-bit operand; they and all leading dimensions at most 2^23.  T < 2^27, segments <= 2^20, adapters <= 65535,
- *                    and the tiles of 32 rows (one more for each segment) times 512 features at most 2^24.
+ *                    and the tiles of 32 rows (one more for each segment) times 512 features at most 2^24 (dA and dB: chunks of rows, at least
+ *                    one for each segment, times 128 features).
  *   base         in  device, bf16, or NULL; may be Z (dX) itself, with the same leading dimension, and must not overlap it otherwise
  *   S, dS        leading dimensions multiples of 4
  *                    No output overlaps anything else.  Inputs must be finite; what is not reaches only the results of its own row (of a row of X, dZ or

@@ -475,10 +475,13 @@ k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, int fblocks, int splits, c
 }
 
 // ---- outer ----------------------------------------------------------------------------------------------------
-// A workgroup of four waves takes 512 features of a chunk of rows of one segment, 128 in a wave, and up to 64 ranks, 32 rows at a time.  Lane (n, q) loads eight features of rows
-// 8 q .. 8 q + 7 (256 bytes of a row in 16 lanes), one step ahead, and transposes them in registers into the operands of eight matrix instructions.
-// L is split into its three parts once per workgroup: each wave prepares one of the operands and leaves it in LDS for the others.
-// The chunk's sum goes to the workspace, and k_adapter_outer_sum adds the chunks of each adapter in order.
+// A workgroup of four waves takes 256 features of a chunk of rows of one segment and up to 64 ranks, 64 rows at a time: a wave 128 features and half the
+// rows.  Lane (n, q) loads eight features of rows 8 q .. 8 q + 7 (256 bytes of a row in 16 lanes), one step ahead, and transposes them in registers into the
+// operands of eight matrix instructions.  L is split into its three parts once per workgroup: each wave prepares its share of the operands and leaves them
+// in LDS for the others; at the end the waves of the same features join their sums there.
+// The chunk's sum goes to the workspace, and k_adapter_outer_sum adds the chunks of each adapter in order.  The sums' bytes are what costs with many ranks:
+// with all four waves on the same rows (512 features, chunks of half the rows for as many workgroups) 7777 ragged rows of 1280 + 5120, rank 64, take 54 us
+// against 47, 32768 rows 131 against 125; rank 16 is the same to 2 %.  Kept in registers, without LDS, L would have to be split by every wave.
 // Both weight gradients are one launch, the workgroups of X before those of dZ.  With more than 64 ranks two workgroups work on the same rows and features,
 // eight apart in the grid, which is the same XCD: the second finds them in its L2.
 struct OuterArgs {
@@ -546,45 +549,54 @@ struct OuterRows {
 };
 template <int RT>
 struct Outer {
-  static_assert(RT <= 4, "a wave prepares one operand of L");
-  static constexpr int LDS = 2 * RT * 3 * 64 * 16;
+  static constexpr int OPS = 2 * RT, PW = (OPS + 3) / 4;                           // operands of L a step, and a wave's share
+  static constexpr int STAGES = 2 * OPS * 3 * 64 * 16, JOIN = 4 * RT * 4 * 64 * 16, LDS = STAGES > JOIN ? STAGES : JOIN;
 
   template <bool BITS8>
   static __device__ __forceinline__ void run(uint8_t* lds, const OuterArgs& a, const Tile& t, int slot, int fb, int rank0, int R) {
-    uint4 (*l)[RT][3][64] = (uint4 (*)[RT][3][64])lds;                             // [buffer][ranks][part][lane]
-    const int lane = (int)threadIdx.x & 63, fw = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int n = lane & 15, q = lane >> 4, f = (fb * 4 + fw) * 128 + n * 8;
+    uint4 (*l)[OPS][3][64] = (uint4 (*)[OPS][3][64])lds;                           // [buffer][rows, ranks][part][lane]
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), fw = wave & 1, rw = wave >> 1;
+    const int n = lane & 15, q = lane >> 4, f = (fb * 2 + fw) * 128 + n * 8;
     const bool in = f < a.C;
     const uint32_t at = in ? (uint32_t)f : kNowhere;
-    const int mine = rank0 + fw * 16 + n;                                          // the rank of L that this lane prepares
     f32x4 acc[RT][8];
 #pragma unroll
     for (int i = 0; i < RT; i++)
 #pragma unroll
       for (int j = 0; j < 8; j++) acc[i][j] = (f32x4){0, 0, 0, 0};
 
-    float v[8];
+    float v[PW][8];
     auto load_l = [&](int r0) {
-      uint32_t q8 = (uint32_t)q * 8;
-      asm("" : "+v"(q8));
-      const BufferRsrc r = rows_of(a.L, t.row + r0, min(t.rows - r0, 32), a.ldl, R);
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[e] = u2f((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)(fw < RT && mine < R ? ((q8 + e) * (uint32_t)a.ldl + (uint32_t)mine) * 4 : kNowhere), 0, 0));
+      for (int p = 0; p < PW; p++) {
+        const int o = wave + 4 * p, first = r0 + o / RT * 32, rank = rank0 + o % RT * 16 + n;
+        uint32_t q8 = (uint32_t)q * 8;
+        asm("" : "+v"(q8));
+        const BufferRsrc r = rows_of(a.L, t.row + first, min(t.rows - first, 32), a.ldl, R);
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          v[p][e] = u2f((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)(o < OPS && rank < R ? ((q8 + e) * (uint32_t)a.ldl + (uint32_t)rank) * 4 : kNowhere), 0, 0));
+      }
     };
     OuterRows<BITS8> m;
     load_l(0);
-    m.load(a, t, 0, at);
+    m.load(a, t, rw * 32, at);
     int buffer = 0;
-    for (int r0 = 0; r0 < t.rows; r0 += 32, buffer ^= 1) {
-      if (fw < RT) split8(v, l[buffer][fw][0][lane], l[buffer][fw][1][lane], l[buffer][fw][2][lane]);
+    for (int r0 = 0; r0 < t.rows; r0 += 64, buffer ^= 1) {
+#pragma unroll
+      for (int p = 0; p < PW; p++) {
+        const int o = wave + 4 * p;
+        if (o < OPS) split8(v[p], l[buffer][o][0][lane], l[buffer][o][1][lane], l[buffer][o][2][lane]);
+      }
       __syncthreads();                                 // nobody comes here before it has read the other buffer, which is written next
       uint4 b[8];
       m.operands(b, a.type);
-      load_l(r0 + 32);
-      m.load(a, t, r0 + 32, at);
+      load_l(r0 + 64);
+      m.load(a, t, r0 + 64 + rw * 32, at);
 #pragma unroll
       for (int i = 0; i < RT; i++) {
-        const uint4 hi = l[buffer][i][0][lane], mid = l[buffer][i][1][lane], lo = l[buffer][i][2][lane];
+        const int o = rw * RT + i;
+        const uint4 hi = l[buffer][o][0][lane], mid = l[buffer][o][1][lane], lo = l[buffer][o][2][lane];
 #pragma unroll
         for (int j = 0; j < 8; j++) {
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(b[j]), acc[i][j], 0, 0, 0);
@@ -593,7 +605,21 @@ struct Outer {
         }
       }
     }
-    // lane (n, q) holds ranks 4 q .. 4 q + 3 of features 8 n .. 8 n + 7
+    // lane (n, q) holds ranks 4 q .. 4 q + 3 of features 8 n .. 8 n + 7; of two waves with the same features each takes half of them
+    f32x4 (*join)[RT * 4][64] = (f32x4 (*)[RT * 4][64])lds;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) join[wave][i * 4 + j][lane] = rw ? acc[i][j] : acc[i][j + 4];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const f32x4 other = join[wave ^ 2][i * 4 + j][lane];
+        acc[i][j] = rw ? other + acc[i][j + 4] : acc[i][j] + other;
+      }
     if (!in) return;
 #pragma unroll
     for (int i = 0; i < RT; i++)
@@ -601,16 +627,15 @@ struct Outer {
       for (int e = 0; e < 4; e++) {
         const int rank = rank0 + i * 16 + 4 * q + e;
         if (rank >= R) continue;
-#pragma unroll
-        for (int h = 0; h < 8; h += 4)
-          *(f32x4*)(a.part + ((int64_t)slot * R + rank) * a.C + f + h) = (f32x4){acc[i][h][e], acc[i][h + 1][e], acc[i][h + 2][e], acc[i][h + 3][e]};
+        *(f32x4*)(a.part + ((int64_t)slot * R + rank) * a.C + f + rw * 4) = (f32x4){acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
       }
   }
 };
 template <int RT>
 __global__ void __launch_bounds__(256, RT == 1 ? 3 : 2)
 k_adapter_outer(AdapterSegments g, OuterArgs x, OuterArgs z, int R, int chunk) {
-  __shared__ __align__(16) uint8_t lds[Outer<RT>::LDS];
+  using O = Outer<RT>;
+  __shared__ __align__(16) uint8_t lds[O::LDS];
   const bool pairs = R > 64;
   const int block = pairs ? (int)blockIdx.x / 16 * 8 + (int)blockIdx.x % 8 : (int)blockIdx.x, rank0 = pairs ? ((int)blockIdx.x / 8 & 1) * 64 : 0;
   const int fblocks = x.fblocks + z.fblocks, slot = uniform(block / fblocks);
@@ -621,8 +646,8 @@ k_adapter_outer(AdapterSegments g, OuterArgs x, OuterArgs z, int R, int chunk) {
   if (second) fb -= x.fblocks;
   const Tile t = find_tile(g, slot, chunk);
   if (t.rows <= 0 || t.adapter < 0) return;
-  if (a.type == M_BF16) Outer<RT>::template run<false>(lds, a, t, slot, fb, rank0, R);
-  else Outer<RT>::template run<true>(lds, a, t, slot, fb, rank0, R);
+  if (a.type == M_BF16) O::template run<false>(lds, a, t, slot, fb, rank0, R);
+  else O::template run<true>(lds, a, t, slot, fb, rank0, R);
 }
 
 struct OuterSum {
@@ -685,7 +710,7 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   ApplyPlan p = {};
   const int64_t extra = (g.segments < g.T ? g.segments : g.T) + 1;     // tiles that segments, and the rows outside them, may add
   const int rank = padded_rank(R);
-  int chunk = down_chunk(rank, 16), chunks = (K + chunk - 1) / chunk;
+  int chunk = down_chunk(rank, 16), chunks = K > 0 ? (K + chunk - 1) / chunk : 1;
   // One launch saves one, about 3 us, and does the first product in 16-row tiles without sharing its contraction out.  Rank 16, 1280 -> 3840: 1 row 5.6
   // against 8.6, 1024 rows 9.2 against 11.2; rank 64, 1280 -> 5120: 512 rows 11.7 against 12.3, 1024 rows 16.7 against 14.9; rank 16, 5120 -> 1280 (20
   // chunks): 64 rows of two segments 8.5 against 9.1, 256 rows of four 11.6 against 9.2, 256 rows of as many 12.7 against 16.5.
@@ -694,6 +719,7 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   if (p.both) {
     const int64_t tiles = g.T / 16 + extra, passes = (C + 1023) / 1024;
     p.slices = (int)(520 / tiles < passes ? 520 / tiles : passes);
+    if (p.slices > (1 << 22) / slots(g, 16)) p.slices = (int)((1 << 22) / slots(g, 16));      // what a grid can count, with a million empty segments
     if (p.slices < 1) p.slices = 1;
     return p;
   }
@@ -744,7 +770,7 @@ void apply(const AdapterApply& a, hipStream_t s) {
 // 512 workgroups 50, 768 47, 1024 55).  A chunk's sum has R / rows times four of its rows' bytes, written and read again: where that gives fewer than 4 R
 // rows (rank 64, 7777 rows of 1280 + 5120: 51 us; 8 R 62), 4 R unless that leaves fewer than 256 workgroups.
 int outer_chunk(int64_t T, int R, int64_t I, int64_t O) {
-  const int64_t blocks = ((I + 511) / 512 + (O + 511) / 512) * (R > 64 ? 2 : 1), least = 4 * padded_rank(R), most = 1 << 20;
+  const int64_t blocks = ((I + 255) / 256 + (O + 255) / 256) * (R > 64 ? 2 : 1), least = 4 * padded_rank(R), most = 1 << 20;
   const auto rows = [&](int64_t workgroups) { return (T * blocks / workgroups + 63) / 64 * 64; };
   int64_t chunk = rows(384);
   if (chunk < least) chunk = rows(256) < least ? rows(256) : least;
@@ -779,7 +805,7 @@ size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, 
 hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOuter& a, const AdapterOuter& b, int accumulate, void* ws, hipStream_t s) {
   const int chunk = outer_chunk(g.T, R, a.C, b.C);
   const auto args = [&](const AdapterOuter& o, float* part) {
-    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + 511) / 512, part};
+    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + 255) / 256, part};
   };
   const OuterArgs x = args(a, (float*)ws), z = args(b, (float*)ws + slots(g, chunk) * R * a.C);
   if (g.T > 0 && x.fblocks + z.fblocks > 0) {

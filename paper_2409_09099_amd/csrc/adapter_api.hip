@@ -151,8 +151,9 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
   TRY(check_matrix(who, "dS", dS, T, R, ldds, 4));
   TRY(check_matrix(who, "dA", dA, adapters * R, I, ldda, 4));
   TRY(check_matrix(who, "dB", dB, adapters * R, O, lddb, 4));
-  if (product_reaches(T / 64 + segments + 2, 2 * (I / 512 + O / 512 + 2), kAdapterMaxGrid)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
-  const size_t need = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
+  const size_t need = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);      // R x (I + O) floats for each chunk
+  if (need > 0 && product_reaches((int64_t)(need / (4 * (size_t)R * (size_t)(I + O))), 2 * (I / 256 + O / 256 + 2), kAdapterMaxGrid))
+    return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SSTE_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, need);
   if (!aligned(workspace, 16)) return fail(SSTE_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);

@@ -63,7 +63,7 @@ WGRAD = [FAKE, 4, 80, 80, 0, 1.0, FAKE, 64, 64, 0, 1.0, None, 0, FAKE, 16, FAKE,
     ({3: 84}, 3), ({8: 68}, 3), ({14: 18}, 3), ({23: 66}, 3), ({25: 82}, 3), ({0: ODD}, 3), ({6: ODD}, 3), ({13: ODD}, 3), ({15: ODD}, 3), ({22: ODD}, 3), ({24: ODD}, 3), ({27: ODD}, 3),
     ({4: 2}, 4), ({4: 4}, 4), ({9: 2}, 4), ({9: 3}, 4), ({5: 2.0}, 5), ({10: 2.0}, 5), ({9: 4, 10: 2.0, 11: FAKE, 12: 2}, 5), ({10: -1.0}, 5), ({26: 2}, 5),
     ({0: None}, 1), ({6: None}, 1), ({13: None}, 1), ({15: None}, 1), ({17: None}, 1), ({22: None}, 1), ({24: None}, 1), ({9: 4, 12: 2}, 1),
-    ({27: None}, 6), ({28: 16}, 6), ({8: HUGE}, 7), ({9: 4, 11: FAKE, 12: HUGE}, 7),
+    ({27: None}, 6), ({28: 16}, 6), ({18: 1 << 20, 2: 1024, 3: 1024, 25: 1024, 7: 1024, 8: 1024, 23: 1024}, 7), ({8: HUGE}, 7), ({9: 4, 11: FAKE, 12: HUGE}, 7),
 ])
 def test_adapter_wgrad_refuses(lib, change, status):
     args = [change.get(i, v) for i, v in enumerate(WGRAD)]

@@ -141,6 +141,19 @@ def test_many_segments(sste, S):
     check_apply(sste, True, T, 64, 64, 8, 9, starts, rng.integers(-1, 9, S).tolist(), "bf16")
 
 
+@pytest.mark.parametrize("T,K,R", [(511, 1280, 16), (512, 1280, 64), (513, 1280, 64), (1024, 1280, 16), (1025, 1280, 16), (64, 5120, 16), (65, 5120, 16), (320, 1024, 128), (647, 1024, 128),
+                                   (8191, 2056, 64), (8192, 2056, 64), (5003, 2056, 128)])
+def test_around_the_plans_ends(sste, T, K, R):
+    """Sizes on both sides of every choice between the ways of sharing the products out."""
+    check_apply(sste, True, T, K, 136, R, 2, [0, T // 3, T], [1, 0], "bf16")
+
+
+def test_a_million_empty_segments(sste):
+    S = 1 << 20
+    for K in (64, 2816):                                                                # in one launch and in two
+        check_apply(sste, True, 1 if K == 64 else 70, K, 7168, 8, 2, [0] * S + [1], [0] * (S - 1) + [1], "bf16")
+
+
 @pytest.mark.parametrize("T", [9, 8200])
 def test_empty(sste, T):
     """No rows, no segments, no adapters, no columns."""
@@ -277,6 +290,9 @@ def check_wgrad(sste, T, I, O, R, N, starts, ids, kind="bf16", x_kind="bf16", ac
     (1000, 128, 264, 128, 4, [0, 500, 900, 1000], [3, 9, 0]),
     (8200, 200, 144, 16, 3, [0, 1, 4000, 8100], [2, 0, 2]),
     (8200, 1032, 72, 48, 1, [0, 8200], [0]),
+    (95, 264, 512, 40, 2, [0, 63, 95], [1, 0]),                    # around the 64 rows of a step, and their halves
+    (97, 256, 520, 72, 2, [0, 32, 97], [1, 0]),
+    (2000, 136, 72, 96, 9, sorted(i * 7919 % 2001 for i in range(201)), [i % 10 for i in range(200)]),
 ])
 def test_wgrad(sste, T, I, O, R, N, starts, ids):
     check_wgrad(sste, T, I, O, R, N, starts, ids)
@@ -433,6 +449,32 @@ def test_other_stream_and_graph(sste):
         torch.cuda.synchronize()
         for n in out:
             assert torch.equal(out[n], want[n]), (k, n)
+
+
+def test_two_streams_at_once(sste):
+    """Two batches on two streams, each with its own workspaces and outputs, the same adapters: as one after the other."""
+    rng = np.random.default_rng(29)
+    T, I, O, R, N = 2500, 2056, 520, 32, 3
+    A, B = normal(rng, (N, R, I), 0.1).to(torch.bfloat16), normal(rng, (N, R, O), 0.1).to(torch.bfloat16)
+    batches = [(normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (T, O), 1).to(torch.bfloat16), *segments([0, n, T - 9], [2, k])) for n, k in ((700, 0), (33, 2))]
+
+    def step(X, dZ, rs, sa):
+        Z, S = sste.adapter_fwd(X, rs, sa, A, B)
+        dX, dS = sste.adapter_dgrad(dZ, rs, sa, A, B)
+        return (Z, S, dX, dS, *sste.adapter_wgrad(dZ, X, S, dS, rs, sa, N))
+
+    want = [step(*b) for b in batches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    got = [[], []]
+    for _ in range(10):
+        for k, (stream, b) in enumerate(zip(streams, batches)):
+            with torch.cuda.stream(stream):
+                got[k].append(step(*b))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for results in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(results, want[k]))
 
 
 def test_layer_with_adapters(sste):
