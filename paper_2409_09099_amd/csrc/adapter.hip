@@ -723,20 +723,26 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
     if (p.slices < 1) p.slices = 1;
     return p;
   }
-  // 64-row tiles read the adapter half as often.  Rank 64, 5120 -> 1280, 16384 rows: 68 against 80, 2999 rows 22.2 against 20.3 (too few tiles); rank 64,
-  // 1024 -> 4096, 8192 rows 44.9 against 44.4 (a short contraction gains nothing); rank 16, 4096 -> 1024, 16384 ragged rows 51 against 46 (a small adapter).
-  const bool wide = rank >= 64;
-  p.large = wide && g.T >= 8192 && (K >= 2048 || g.T >= 32768);
-  // The contraction is shared out, in whole chunks and at least four of them, until there are about 512 workgroups with many ranks, 1024 with few: rank 64,
-  // 2999 ragged rows of 5120: 21.6 in four, 24 in three, 31 in one; rank 16, 16384 ragged rows of 4096: 51 in one, 47 in two, 46 in three.
-  chunk = down_chunk(rank, p.large ? 64 : 32), chunks = (K + chunk - 1) / chunk;
-  const int64_t tiles = g.T / (p.large ? 64 : 32) + extra;
-  int64_t splits = ((wide ? 512 : 1024) + tiles / 2) / tiles;
-  if (splits > chunks / 4) splits = chunks / 4;
-  if (splits > kMostSplits) splits = kMostSplits;
-  if (splits < 1 || !workspace) splits = 1;
-  p.span = (int)((chunks + splits - 1) / splits * chunk);
-  p.splits = chunks > 0 ? (K + p.span - 1) / p.span : 1;
+  // Tiles of 32 or 64 rows, which read the adapter half as often, and the contraction shared out in up to four, in whole chunks and at least four of them:
+  // the least of what the first product loads, rows counted twice (they come from memory, the adapter from L2), by rounds of a workgroup on every CU, the
+  // last as if half full, a workgroup as if three chunks longer than it is; and, with partial sums, of their writes and of each block of features reading
+  // them.  The factors are fitted to 310 problems (ranks 16 to 128, bf16 and e4m3, 1280 ... 5120 wide, 700 ... 32768 rows): the choice costs 0.9 % over the
+  // best of the eight ways in the mean, 14 % at most, where limits on rows, ranks and widths cost 5 % and 25 %.  Rank 128, 5003 ragged rows, 1280 -> 3840:
+  // 38.1 us in one part, 42.2 in two, 47.9 in four; 3840 -> 1280: 35.0, 33.8, 32.5, and 28.9 in two of 64-row tiles.
+  double best = 0;
+  for (int rows = 32; rows <= 64; rows += 32) {
+    chunk = down_chunk(rank, rows), chunks = K > 0 ? (K + chunk - 1) / chunk : 1;
+    const int64_t tiles = g.T / rows + extra;
+    for (int want = 1; want <= (workspace ? kMostSplits : 1) && (want == 1 || want <= chunks / 4); want++) {
+      const int each = (chunks + want - 1) / want, splits = (chunks + each - 1) / each;
+      const double rounds = (double)(tiles * splits) / 256, whole = (double)((tiles * splits + 255) / 256), full = (rounds + whole) / 2;
+      const double loads = (full < 1 ? 1 : full) * (each + 3) * chunk * (2 * rows + rank);
+      const double sums = splits > 1 ? 0.0148 * splits * (double)g.T * R * (1 + (C + 511) / 512) : 0;
+      if (best > 0 && loads + sums >= best) continue;
+      best = loads + sums;
+      p.large = rows == 64, p.splits = splits, p.span = each * chunk;
+    }
+  }
   return p;
 }
 
