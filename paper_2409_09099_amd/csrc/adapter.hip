@@ -723,21 +723,22 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
     if (p.slices < 1) p.slices = 1;
     return p;
   }
-  // Tiles of 32 or 64 rows, which read the adapter half as often, and the contraction shared out in up to four, in whole chunks and at least four of them:
-  // the least of what the first product loads, rows counted twice (they come from memory, the adapter from L2), by rounds of a workgroup on every CU, the
-  // last as if half full, a workgroup as if three chunks longer than it is; and, with partial sums, of their writes and of each block of features reading
-  // them.  The factors are fitted to 310 problems (ranks 16 to 128, bf16 and e4m3, 1280 ... 5120 wide, 700 ... 32768 rows): the choice costs 0.9 % over the
-  // best of the eight ways in the mean, 14 % at most, where limits on rows, ranks and widths cost 5 % and 25 %.  Rank 128, 5003 ragged rows, 1280 -> 3840:
-  // 38.1 us in one part, 42.2 in two, 47.9 in four; 3840 -> 1280: 35.0, 33.8, 32.5, and 28.9 in two of 64-row tiles.
+  // Tiles of 32 or 64 rows, which read the adapter half as often (not of rank 16, whose adapters are small: 16384 rows of 4096 48.7 us against 57), and the
+  // contraction shared out in up to four, in whole chunks and at least four of them: the least of what the first product loads, rows counted twice (they come
+  // from memory, the adapter from L2), by rounds of a workgroup on every CU, the last as if half full, a workgroup as if 256 elements longer than it is; and,
+  // with partial sums, of their writes and of each block of features reading them.  The factors are fitted to 446 problems (ranks 8 to 128, bf16 and e4m3,
+  // 1280 ... 5120 wide, 700 ... 32768 rows): the choice costs 1.1 % over the best of the eight ways in the mean, 14 % at most, where limits on rows, ranks and
+  // widths cost 4 % and 25 %.  Rank 128, 5003 ragged rows, 1280 -> 3840: 38.1 us in one part, 42.2 in two, 47.9 in four; 3840 -> 1280: 35.0, 33.8, 32.5, and
+  // 28.9 in two of 64-row tiles.
   double best = 0;
-  for (int rows = 32; rows <= 64; rows += 32) {
+  for (int rows = 32; rows <= (rank > 16 ? 64 : 32); rows += 32) {
     chunk = down_chunk(rank, rows), chunks = K > 0 ? (K + chunk - 1) / chunk : 1;
     const int64_t tiles = g.T / rows + extra;
     for (int want = 1; want <= (workspace ? kMostSplits : 1) && (want == 1 || want <= chunks / 4); want++) {
       const int each = (chunks + want - 1) / want, splits = (chunks + each - 1) / each;
       const double rounds = (double)(tiles * splits) / 256, whole = (double)((tiles * splits + 255) / 256), full = (rounds + whole) / 2;
-      const double loads = (full < 1 ? 1 : full) * (each + 3) * chunk * (2 * rows + rank);
-      const double sums = splits > 1 ? 0.0148 * splits * (double)g.T * R * (1 + (C + 511) / 512) : 0;
+      const double loads = (full < 1 ? 1 : full) * ((double)each * chunk + 256) * (2 * rows + rank);
+      const double sums = splits > 1 ? 0.012 * splits * (double)g.T * R * (1 + (C + 511) / 512) : 0;
       if (best > 0 && loads + sums >= best) continue;
       best = loads + sums;
       p.large = rows == 64, p.splits = splits, p.span = each * chunk;
@@ -756,7 +757,7 @@ void apply(const AdapterApply& a, hipStream_t s) {
     return;
   }
   const dim3 grid((unsigned)(slots(a.seg, p.large ? 64 : 32) * p.splits));
-  if (p.large) SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, 4>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
+  if (RP > 16 && p.large) SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, (RP > 16 ? RP / 16 : 2), 4>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
   else SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, 2>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
   const int fblocks = a.C > 0 ? (a.C + 511) / 512 : 1;               // without features D is still to be added up
   if (a.C > 0 || p.splits > 1)
