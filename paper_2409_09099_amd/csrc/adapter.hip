@@ -140,6 +140,8 @@ __device__ __forceinline__ void buffer_store_b128(BufferRsrc r, uint32_t voffset
 // of the rows and of the adapter, loaded in whole pieces of a row (the operands' own layout has a different row in every lane, at a quarter of the load
 // rate) and kept two chunks ahead in registers.  A wave multiplies one step of 32 elements of each chunk; where a chunk has fewer steps than there are
 // waves, the waves share the ranks out as well.  The sums of the steps' waves meet in LDS, in the order of the steps.
+// Bound by HBM with few ranks (32768 e4m3 rows of 1280, rank 32: 17 us, 2.7 TB/s, the read of X and the write of D; 16384 bf16
+// rows of 4096, rank 16: 30 us, 4.5 TB/s), by the adapter's way through L2 and LDS with many (5003 e5m2 rows of 3840, rank 128: 17 us).
 // Elements of a chunk: as many as leave room for two or three workgroups a CU; for few rows, where the chunks' latency adds up, twice as many for rank 32 (one
 // row of 1280 -> 3840: 5.7 us against 9.6) and 128 (one row of 1280 -> 1280: 10.5 against 12.1), not for 64 (64 rows of their own 16.1, against 20.8).
 constexpr int down_chunk(int padded_rank, int rows) {
@@ -375,7 +377,8 @@ __device__ __forceinline__ void bare_features(const Tile& t, int f0, int C, cons
 
 __device__ __forceinline__ float scale_of(const DownArgs& a, const Tile& t) { return (a.scale ? a.scale[t.adapter] : 1.0f) * a.x_scale; }
 
-// Both products of 16 rows in one launch, for few rows: `slices` workgroups share a tile's features, and each computes D for itself.
+// Both products of 16 rows in one launch, for few rows, bound by the launch and four waits for memory in a row (the bounds, the first chunk, the features'
+// ranks, the stores; one row of 1280 -> 3840, rank 16: 5.5 us; 96 rows of 64 adapters, 1280 -> 5120: 8.9 us, 1.7 TB/s): `slices` workgroups share a tile's features, and each computes D for itself.
 template <int DT, int RT>
 __global__ void __launch_bounds__(512)
 k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, int slices) {
@@ -431,7 +434,8 @@ k_adapter_down(AdapterSegments g, DownArgs d, int splits, int span, float* __res
   }
 }
 
-// Up alone, 512 features of a tile's rows in a workgroup of four waves.  splits > 1: adds the splits' sums in order and scales them; the workgroups of
+// Up alone, 512 features of a tile's rows in a workgroup of four waves.  Bound by HBM, base read and out written (32768 rows of 5120, rank 32: 117 us, 5.8 TB/s;
+// 16384 rows of 1024, rank 16, with two partial sums: 15.5 us, 4.5 TB/s), with rank 128 by the adapter's way through L2 too (5003 rows of 1280: 13.5 us).  splits > 1: adds the splits' sums in order and scales them; the workgroups of
 // the first features write D.
 template <int RP, int TT>
 __global__ void __launch_bounds__(256, RP <= 32 ? 3 : 2)
@@ -482,6 +486,8 @@ k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, int fblocks, int splits, c
 // The chunk's sum goes to the workspace, and k_adapter_outer_sum adds the chunks of each adapter in order.  The sums' bytes are what costs with many ranks:
 // with all four waves on the same rows (512 features, chunks of half the rows for as many workgroups) 7777 ragged rows of 1280 + 5120, rank 64, take 54 us
 // against 47, 32768 rows 131 against 125; rank 16 is the same to 2 %.  Kept in registers, without LDS, L would have to be split by every wave.
+// Bound by HBM with few ranks (16384 rows of 1024 + 4096, rank 16: 40 us, 4.2 TB/s, and 5.5 for the sums), by the sums' bytes and, from rank 64 on, the matrix
+// instructions of three parts (16384 rows of 1280 + 5120, rank 128: 105 us, 80 GFLOP of them).
 // Both weight gradients are one launch, the workgroups of X before those of dZ.  With more than 64 ranks two workgroups work on the same rows and features,
 // eight apart in the grid, which is the same XCD: the second finds them in its L2.
 struct OuterArgs {
@@ -657,7 +663,7 @@ struct OuterSum {
   float scale;
   int C;
 };
-// Adds the chunks of adapter n in the order of their rows.
+// Adds the chunks of adapter n in the order of their rows.  Bound by the reads, which mostly come from the last-level cache (34 MB in 9 us).
 __global__ void __launch_bounds__(256)
 k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b, int ablocks, int accumulate) {
   const bool second = (int)blockIdx.x >= ablocks;
@@ -773,9 +779,10 @@ void apply(const AdapterApply& a, hipStream_t s) {
   }
 }
 
-// Rows of a chunk of the weight gradients: about 384 workgroups of 512 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 43 us;
-// 512 workgroups 50, 768 47, 1024 55).  A chunk's sum has R / rows times four of its rows' bytes, written and read again: where that gives fewer than 4 R
-// rows (rank 64, 7777 rows of 1280 + 5120: 51 us; 8 R 62), 4 R unless that leaves fewer than 256 workgroups.
+// Rows of a chunk of the weight gradients: about 384 workgroups of 256 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 44.4 us;
+// 256 workgroups 50.2, 512 46.7; 7777 ragged rows of 1280 + 5120, rank 64: 47.0, 52.1 and 54.2).  A chunk's sum has R / rows times four of its rows' bytes,
+// written and read again: where 384 give fewer than 4 R rows (rank 64, 4096 rows of 1280 + 1280: 19.6 us, with half of them 23.2), 4 R unless that leaves
+// fewer than 256 workgroups.
 int outer_chunk(int64_t T, int R, int64_t I, int64_t O) {
   const int64_t blocks = ((I + 255) / 256 + (O + 255) / 256) * (R > 64 ? 2 : 1), least = 4 * padded_rank(R), most = 1 << 20;
   const auto rows = [&](int64_t workgroups) { return (T * blocks / workgroups + 63) / 64 * 64; };

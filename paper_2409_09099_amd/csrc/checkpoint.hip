@@ -4,7 +4,9 @@
 //   backward  h = code * 2^e, A = act(h), dH = dA * act'(h)
 //
 // A power of two makes both directions exact but for the one rounding to e4m3, and a block of 32 keeps a feature with large values from
-// taking the others' bits.  Both passes read every element once and write once: bound by memory traffic.
+// taking the others' bits.  Both passes read every element once and write once: bound by memory traffic.  32768 x 5120: pack 92 us, 5.5 TB/s; 16384 x 5120:
+// backward with GELU, its derivative and dA 113 us, 5.2 TB/s (a copy on the same card: 5.1).  333 x 1280 takes 3.2 us, a launch.
+// A thread's two pieces a pass are loaded before either is converted.
 #include "adapter.h"
 
 namespace sste {
