@@ -63,6 +63,28 @@ __device__ __forceinline__ Tile find_tile(const AdapterSegments& g, int slot, in
   t.adapter = __builtin_amdgcn_readlane(adapter, hit);
   return t;
 }
+// Workgroups go to the eight XCDs in turn: `grouped`, the `parts` of a slot are on one of them, whose L2 has what they share after the first (slots are
+// rounded up to a multiple of eight, and the last may be empty).
+struct Share {
+  int parts;
+  bool grouped;
+  uint32_t magic;       // i / parts = i * magic >> shift for i < 2^25
+  int shift;
+};
+Share share_of(int parts, bool grouped) {
+  int bits = 0;
+  while ((1 << bits) < parts) bits++;
+  return {parts, grouped, (uint32_t)(((1ull << (25 + bits)) + parts - 1) / parts), 25 + bits};
+}
+struct Work {
+  int slot, part;
+};
+// (All of it in scalar registers: a division would go through vector registers, and its results back.)
+__device__ __forceinline__ Work work_of(Share s) {
+  const int shift = s.grouped ? 3 : 0, i = (int)blockIdx.x >> shift, group = (int)((uint64_t)(uint32_t)i * s.magic >> s.shift);
+  return {(group << shift) + ((int)blockIdx.x - (i << shift)), i - group * s.parts};
+}
+unsigned grid_of(int64_t slots, Share s) { return (unsigned)((s.grouped ? (slots + 7) / 8 * 8 : slots) * s.parts); }
 int64_t slots(const AdapterSegments& g, int tr) { return (int64_t)g.T / tr + g.segments + 2; }
 
 // ---- operands -------------------------------------------------------------------------------------------------
@@ -380,13 +402,14 @@ __device__ __forceinline__ float scale_of(const DownArgs& a, const Tile& t) { re
 // Both products of 16 rows in one launch, for few rows, bound by the launch and four waits for memory in a row (the bounds, the first chunk, the features'
 // ranks, the stores; one row of 1280 -> 3840, rank 16: 5.5 us; 96 rows of 64 adapters, 1280 -> 5120: 8.9 us, 1.7 TB/s): `slices` workgroups share a tile's features, and each computes D for itself.
 template <int DT, int RT>
-__global__ void __launch_bounds__(512)
-k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, int slices) {
+__global__ void __launch_bounds__(512, RT <= 4 ? 4 : 2)      // two workgroups a CU up to rank 64 (200 rows of their own, 2560 -> 2560: 23.4 us against 29.4)
+k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, Share share) {
   using D = Down<DT, RT, 1>;
   __shared__ __align__(16) uint8_t lds[D::LDS];
   __shared__ __align__(16) Up<RT * 16, 1> up;
-  const int slot = uniform((int)blockIdx.x / slices), slice = (int)blockIdx.x - slot * slices;
-  const Tile t = find_tile(g, slot, 16);
+  const Work w = work_of(share);
+  const int slice = w.part, slices = share.parts;
+  const Tile t = find_tile(g, w.slot, 16);
   if (t.rows <= 0) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (t.adapter < 0) {
@@ -439,10 +462,11 @@ k_adapter_down(AdapterSegments g, DownArgs d, int splits, int span, float* __res
 // the first features write D.
 template <int RP, int TT>
 __global__ void __launch_bounds__(256, RP <= 32 ? 3 : 2)
-k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, int fblocks, int splits, const float* __restrict__ part) {
+k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, Share share, int splits, const float* __restrict__ part) {
   __shared__ __align__(16) Up<RP, TT> up;
-  const int slot = uniform((int)blockIdx.x / fblocks), fb = (int)blockIdx.x - slot * fblocks;
-  const Tile t = find_tile(g, slot, TT * 16);
+  const Work w = work_of(share);
+  const int fb = w.part;
+  const Tile t = find_tile(g, w.slot, TT * 16);
   if (t.rows <= 0) return;
   const int f = (fb * 4 + ((int)threadIdx.x >> 6)) * 128;
   if (t.adapter < 0) {
@@ -708,7 +732,7 @@ int padded_rank(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128
 // How the two products of a call are shared out.  Times are of both kernels, or of the one, in us.
 struct ApplyPlan {
   bool both;         // one launch
-  int slices;        // of it: workgroups of a tile
+  Share share;       // of it or of the second: workgroups of a tile
   bool large;        // two launches: tiles of 64 rows for the first, otherwise of 32
   int splits, span;  // of its contraction
 };
@@ -722,11 +746,14 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   // chunks): 64 rows of two segments 8.5 against 9.1, 256 rows of four 11.6 against 9.2, 256 rows of as many 12.7 against 16.5.
   const bool single = 2 * (int64_t)g.segments >= g.T;                  // mostly one row a segment: tiles are as good as empty whatever their size
   p.both = (int64_t)g.T * chunks <= 5120 && (chunks <= 10 || g.T <= 64 || single);
+  const int64_t all = g.T / (p.both ? 16 : 32) + extra;
   if (p.both) {
-    const int64_t tiles = g.T / 16 + extra, passes = (C + 1023) / 1024;
-    p.slices = (int)(520 / tiles < passes ? 520 / tiles : passes);
-    if (p.slices > (1 << 22) / slots(g, 16)) p.slices = (int)((1 << 22) / slots(g, 16));      // what a grid can count, with a million empty segments
-    if (p.slices < 1) p.slices = 1;
+    // A tile's workgroups read the same rows and the same adapter: on one XCD (rank 16, 2560 -> 2560, 200 rows of 6 segments 6.0 us against 7.9; 96 of 96, 1280
+    // -> 3840, 8.2 against 8.7, though -> 5120 9.9 against 9.2), unless some XCDs would have no tile (rank 128, 1280 -> 5120, 1 row: 13.1 against 10.7).
+    const int64_t passes = C > 0 ? (C + 1023) / 1024 : 1, most = (1 << 22) / (slots(g, 16) + 8);      // what a grid can count, with a million empty segments
+    int64_t slices = 520 / all < passes ? 520 / all : passes;
+    if (slices > most) slices = most;
+    p.share = share_of((int)(slices < 1 ? 1 : slices), all >= 8);
     return p;
   }
   // Tiles of 32 or 64 rows, which read the adapter half as often (not of rank 16, whose adapters are small: 16384 rows of 4096 48.7 us against 57), and the
@@ -750,6 +777,10 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
       p.large = rows == 64, p.splits = splits, p.span = each * chunk;
     }
   }
+  // The workgroups of the second share a tile's D and its partial sums: on one XCD (rank 128, 1280 -> 3840, 1500 rows in three: 17.7 us against 21.6; rank 64,
+  // 32768 rows in one 129 against 133) where these are many; with few the order of the rows in memory counts for more (rank 32, 1280 -> 5120, 32768 rows:
+  // 135.5 against 132).
+  p.share = share_of(C > 0 ? (C + 511) / 512 : 1, all >= 8 && rank * p.splits >= 64);      // without features D is still to be added up
   return p;
 }
 
@@ -759,15 +790,14 @@ void apply(const AdapterApply& a, hipStream_t s) {
   const DownArgs d = {(const uint8_t*)a.X, a.ldx, a.K, (const uint16_t*)a.down, a.lddown, a.R, a.scale, a.x_scale, a.D, a.ldd};
   const UpArgs o = {(const uint16_t*)a.up, a.ldup, a.C, (const uint16_t*)a.base, a.ldbase, (uint16_t*)a.out, a.ldout};
   if (p.both) {
-    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_both<DT, RP / 16>), dim3((unsigned)(slots(a.seg, 16) * p.slices)), dim3(512), s, a.seg, d, o, p.slices);
+    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_both<DT, RP / 16>), dim3(grid_of(slots(a.seg, 16), p.share)), dim3(512), s, a.seg, d, o, p.share);
     return;
   }
   const dim3 grid((unsigned)(slots(a.seg, p.large ? 64 : 32) * p.splits));
   if (RP > 16 && p.large) SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, (RP > 16 ? RP / 16 : 2), 4>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
   else SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_down<DT, RP / 16, 2>), grid, dim3(512), s, a.seg, d, p.splits, p.span, a.ws);
-  const int fblocks = a.C > 0 ? (a.C + 511) / 512 : 1;               // without features D is still to be added up
   if (a.C > 0 || p.splits > 1)
-    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_up<RP, 2>), dim3((unsigned)(slots(a.seg, 32) * fblocks)), dim3(256), s, a.seg, d, o, fblocks, p.splits, a.ws);
+    SSTE_LAUNCH(SSTE_K_ADAPTER, (k_adapter_up<RP, 2>), dim3(grid_of(slots(a.seg, 32), p.share)), dim3(256), s, a.seg, d, o, p.share, p.splits, a.ws);
 }
 template <int DT>
 void apply(const AdapterApply& a, hipStream_t s) {
