@@ -144,6 +144,8 @@ def _matrix(t: torch.Tensor, itemsize: int, name: str) -> Tuple[int, int, int]:
         raise ValueError(f"{name} must have {itemsize}-byte elements")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have unit stride along its last axis")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows must not overlap (an expanded tensor needs .contiguous())")
     ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0) if t.shape[0] == 1 else t.shape[1])
     return t.shape[0], t.shape[1], max(ld, t.shape[1])
 
@@ -516,8 +518,12 @@ def _together(first: torch.Tensor, *others: Optional[torch.Tensor]) -> "torch.cu
     return torch.cuda.device(first.device)
 
 
-def _bytes(t: Optional[torch.Tensor]) -> int:
-    return t.numel() * t.element_size() if t is not None else 0
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    if workspace is None:
+        return 0
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
 
 
 def adapter_workspace_bytes(T: int, segments: int, R: int, width_in: int, width_out: int) -> int:

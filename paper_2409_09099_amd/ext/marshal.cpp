@@ -130,6 +130,7 @@ Matrix matrix(Args& a, const at::Tensor* t, int itemsize) {
   if (t->dim() != 2 || !t->is_cuda() || (int)t->element_size() != itemsize || (t->size(1) > 1 && t->stride(1) != 1)) return a.ok = false, m;
   m.rows = t->size(0);
   m.cols = t->size(1);
+  if (m.rows > 1 && t->stride(0) < m.cols) return a.ok = false, m;      // an expanded tensor, or a window over itself
   m.ld = m.rows >= 1 ? std::max(m.cols, t->stride(0)) : m.cols;
   m.p = t->numel() > 0 ? t->data_ptr() : nullptr;
   return m;
@@ -146,6 +147,7 @@ Stack stack(Args& a, const at::Tensor* t, int itemsize) {
   m.n = t->size(0);
   m.rank = t->size(1);
   m.width = t->size(2);
+  if (m.rank > 1 && t->stride(1) < m.width) return a.ok = false, m;
   m.ld = m.n >= 1 && m.rank >= 1 ? std::max(m.width, t->stride(1)) : m.width;
   if (m.n > 1 && t->stride(0) != m.rank * m.ld) a.ok = false;
   m.p = t->numel() > 0 ? t->data_ptr() : nullptr;
@@ -414,6 +416,7 @@ PyObject* adapter(Fn f, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnam
   if (a.ok && !Z) made_z = make(*X, x.rows, C, at::kBFloat16);
   if (a.ok && !S) made_s = make(*X, x.rows, ma.rank, at::kFloat);
   together(a, X, {rs, sa, A, B, scale, base, Z, S, ws});
+  if (ws && !ws->is_contiguous()) a.ok = false;
   const Matrix z = exactly(a, Z ? Z : &made_z, x.rows, C, at::kBFloat16), sm = exactly(a, S ? S : &made_s, x.rows, ma.rank, at::kFloat);
   if (!a.ok) return decline(f, args, nargs, kwnames);
   at::Tensor scratch;
@@ -480,6 +483,7 @@ PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
   if (!dB) made_b = at::empty({n, R, y.cols}, f32), dB = &made_b;
   const Stack ga = stack(a, dA, 4), gb = stack(a, dB, 4);
   together(a, dZ, {X, S, dS, rs, sa, xdt == SSTE_F8BLOCK ? xb : nullptr, dA, dB, ws});
+  if (ws && !ws->is_contiguous()) a.ok = false;
   if (!a.ok || dA->scalar_type() != at::kFloat || dB->scalar_type() != at::kFloat || ga.n != n || gb.n != n || ga.rank != R || gb.rank != R || ga.width != x.cols || gb.width != y.cols)
     return decline(ADAPTER_WGRAD, args, nargs, kwnames);
   if (!ws) {

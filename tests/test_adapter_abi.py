@@ -134,3 +134,15 @@ def test_binding_refuses():
                  lambda: sste.adapter_fwd(z(4), i(0, 4), i(0), z(1, 8, 64), z(1, 8, 80))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_refuses_overlapping_rows():
+    """Rows that share memory (an expanded tensor) have no leading dimension; told by shape and strides alone."""
+    from types import SimpleNamespace
+    from paper_2409_09099_amd import binding
+    like = lambda shape, strides: SimpleNamespace(dim=lambda: len(shape), is_cuda=True, element_size=lambda: 2, shape=shape, stride=lambda i: strides[i])      # noqa: E731
+    for strides in ((0, 1), (63, 1), (8, 1)):
+        with pytest.raises(ValueError):
+            binding._matrix(like((4, 64), strides), 2, "X")
+    assert binding._matrix(like((4, 64), (64, 1)), 2, "X") == (4, 64, 64) and binding._matrix(like((1, 64), (0, 1)), 2, "X") == (1, 64, 64)
+    assert binding._matrix(like((0, 64), (0, 1)), 2, "X") == (0, 64, 64) and binding._matrix(like((4, 0), (1, 1)), 2, "X")[:2] == (4, 0)

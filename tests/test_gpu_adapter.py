@@ -373,6 +373,9 @@ def test_native_marshalling(sste):
                  lambda: sste.adapter_dgrad(X, *seg, A, B), lambda: sste.adapter_wgrad(dZ[:9], X, S, S, *seg, N), lambda: sste.adapter_wgrad(dZ, X, S, S[:, :8], *seg, N),
                  lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, accumulate=True), lambda: sste.adapter_wgrad(dZ, codes, S, S, *seg, N, x_dtype=sste.F8BLOCK),
                  lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, dA=torch.zeros((N, R, I + 8), device="cuda")),
+                 lambda: sste.adapter_fwd(X[:1].expand(T, I), *seg, A, B), lambda: sste.adapter_fwd(X, *seg, A[:, :1].expand(N, R, I), B), lambda: sste.adapter_fwd(X, *seg, A[:1].expand(N, R, I), B),
+                 lambda: sste.adapter_fwd(X, *seg, A, B, base=base[:1].expand(T, O)), lambda: sste.adapter_wgrad(dZ[:1].expand(T, O), X, S, S, *seg, N), lambda: sste.checkpoint_pack(X[:1].expand(T, I)),
+                 lambda: sste.adapter_fwd(X, *seg, A, B, workspace=codes[:1, :1].expand(1 << 20, 1)), lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, workspace=codes[:1, :1].expand(1 << 20, 1)),
                  lambda: sste.checkpoint_pack(X, codes=codes[:9]), lambda: sste.checkpoint_pack(X, scales=torch.empty((T, 4), dtype=i32, device="cuda")),
                  lambda: sste.checkpoint_backward(codes, blocks[:, :2]), lambda: sste.checkpoint_backward(codes, blocks, dH=X), lambda: sste.checkpoint_backward(codes, blocks, A=X, restore=False)):
         with pytest.raises(ValueError):
