@@ -63,7 +63,7 @@ static int apply(const char* who, const char* xname, const char* dname, const ch
   if (a.base) TRY(check_matrix(who, "base", a.base, T, C, a.ldbase, 8));
   if (a.base == a.out && a.base && T > 1 && a.ldbase != a.ldout) return fail(SSTE_ERR_VALUE, "%s: base may be %s itself only with the same leading dimension", who, oname);
   if (!aligned(a.scale, 4)) return fail(SSTE_ERR_ALIGN, "%s: scale must be 4-byte aligned", who);
-  if (product_reaches(T / 32 + segments + 2, (C + 511) / 512, kAdapterMaxGrid)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
+  if (product_reaches(T / 32 + segments + 9, (C + 511) / 512, kAdapterMaxGrid)) return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
   // without the workspace (none, too small, misaligned) the contraction is not split: the same function, slower for few rows
   const size_t need = adapter_apply_workspace_bytes(T, (int)segments, (int)R, K, C);
   a.ws = ws && ws_bytes >= need && need > 0 && aligned(ws, 16) ? (float*)ws : nullptr;

@@ -36,6 +36,7 @@ FWD = [FAKE, 4, 64, 64, 0, 1.0, FAKE, 2, FAKE, FAKE, 64, FAKE, 80, FAKE, 3, 16, 
     ({0: None}, 1), ({6: None}, 1), ({8: None}, 1), ({9: None}, 1), ({11: None}, 1), ({19: None}, 1), ({21: None}, 1),
     ({4: 1, 2: 72, 3: 80, 10: 72}, 7), ({4: 1, 2: 64, 3: 72}, 3),          # 8-bit rows are multiples of 16
     ({3: HUGE}, 7), ({20: HUGE}, 7), ({22: HUGE}, 7), ({10: HUGE}, 7),
+    ({1: 2040, 7: 953, 16: 1 << 23, 12: 1 << 23, 18: 1 << 23, 20: 1 << 23}, 7),          # tiles that a grid, rounded up to the XCDs, cannot count
 ])
 def test_adapter_fwd_refuses(lib, change, status):
     args = [change.get(i, v) for i, v in enumerate(FWD)]
