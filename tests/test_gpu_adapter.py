@@ -415,10 +415,11 @@ def test_gradients_against_differences(sste):
             assert abs((up - down) - g[at]) <= step * np.abs(g).max() + 1e-9 * abs(up), (name, at)
 
 
-def test_other_stream_and_graph(sste):
+@pytest.mark.parametrize("T,I,O,R", [(300, 136, 264, 16), (2500, 2056, 520, 64)])          # one launch a product; shared out, with workspaces of the graph's own
+def test_other_stream_and_graph(sste, T, I, O, R):
     """Captured once, replayed with other segments, adapters and rows written into the same tensors, between eager work."""
     rng = np.random.default_rng(11)
-    T, I, O, R, N = 300, 136, 264, 16, 4
+    N = 4
     X, dZ, base = (normal(rng, (T, n), 1).to(torch.bfloat16) for n in (I, O, O))
     A, B = normal(rng, (N, R, I), 0.1).to(torch.bfloat16), normal(rng, (N, R, O), 0.1).to(torch.bfloat16)
     rs, sa = segments([0, 100, 200, 300], [0, 1, 2])
