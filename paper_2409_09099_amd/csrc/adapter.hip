@@ -556,6 +556,22 @@ struct OuterRows {
         e[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rs, (int)(f == kNowhere ? f : (q8 + i) * (uint32_t)a.ldblocks + (f >> 5)), 0, 0);
     }
   }
+  // Rows of a list; `f` is a feature that there is
+  __device__ __forceinline__ void load(const OuterArgs& a, const int* rows, int f) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int64_t row = rows[i];
+      if constexpr (BITS8) {
+        const uint2 v = *(const uint2*)(a.M + row * a.ldm + f);
+        x[i][0] = v.x, x[i][1] = v.y;
+        e[i] = 127;
+        if (a.type == M_BLOCK) e[i] = a.blocks[row * a.ldblocks + (f >> 5)];
+      } else {
+        const uint4 v = *(const uint4*)(a.M + (row * a.ldm + f) * 2);
+        x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
+      }
+    }
+  }
   // b[j]: rows 0 .. 7 of feature j
   __device__ __forceinline__ void operands(uint4 (&b)[8], int type) const {
     if constexpr (!BITS8) transpose_rows(x, b);
@@ -726,6 +742,121 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
   *(f32x4*)p = sum;
 }
 
+// Both weight gradients of few rows in one launch: a workgroup takes 128 features of one adapter, 16 ranks, and all rows that the adapter has, 32 in each of
+// eight waves at a time.  The rows are listed in LDS first, in order, by a search of every row's segment, so that an adapter's short segments share a step; behind the
+// last the list repeats it, with zeros of L.  The waves' sums meet in LDS, in the order of the rows.
+// Bound by the launch and the waits in a row: the bounds, the rows of L and M, the stores.
+constexpr int kFewRows = 2048, kFewSegments = 256;
+struct RowList {
+  int start[kFewSegments + 1], adapter[kFewSegments], counts[kFewRows / 64];
+  int rows[kFewRows + 8];
+
+  // Lists the rows of adapter n and returns their number.
+  __device__ __forceinline__ int find(const AdapterSegments& g, int n) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    bool some = false;
+    if (tid < g.segments) {
+      const int v = g.adapter[tid];
+      start[tid] = g.row_start[tid];
+      adapter[tid] = v;
+      some = v == n;
+      if (tid == g.segments - 1) start[tid + 1] = g.row_start[tid + 1];
+    }
+    if (!__syncthreads_or(some)) return 0;
+    uint64_t mine[kFewRows / 512];
+#pragma unroll
+    for (int j = 0; j < kFewRows / 512; j++) {
+      mine[j] = 0;
+      if (j * 512 < g.T) {
+        const int row = j * 512 + tid;
+        int lo = 0;                                    // segment lo - 1 is the last that starts at the row or before it, if lo > 0
+        for (int step = 1 << (31 - __builtin_clz(g.segments)); step > 0; step >>= 1)
+          if (lo + step <= g.segments && start[lo + step - 1] <= row) lo += step;
+        mine[j] = __ballot(row < g.T && lo > 0 && row < start[lo] && adapter[max(lo - 1, 0)] == n);
+      }
+      if (lane == 0) counts[j * 8 + wave] = __popcll(mine[j]);
+    }
+    __syncthreads();
+    int total = 0, at[kFewRows / 512];
+#pragma unroll
+    for (int k = 0; k < kFewRows / 64; k++) {
+      if (k % 8 == wave) at[k / 8] = total;
+      total += counts[k];
+    }
+#pragma unroll
+    for (int j = 0; j < kFewRows / 512; j++)
+      if (mine[j] >> lane & 1) {
+        const int to = at[j] + __popcll(mine[j] & ((1ull << lane) - 1));
+        rows[to] = j * 512 + tid;
+        if (to == total - 1)
+          for (int i = 1; i < 8; i++) rows[to + i] = j * 512 + tid;
+      }
+    __syncthreads();
+    return uniform(total);
+  }
+};
+struct OuterFew {
+  RowList list;
+  f32x4 join[8][8][64];
+
+  template <bool BITS8>
+  __device__ __forceinline__ void run(int count, const OuterArgs& a, const OuterSum& s, int n, int fb, int rank0, int R, int accumulate) {
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int m = lane & 15, q = lane >> 4, f = fb * 128 + m * 8, rank = min(rank0 + m, R - 1);
+    f32x4 acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) acc[j] = (f32x4){0, 0, 0, 0};
+    for (int at = wave * 32 + q * 8, r0 = wave * 32; r0 < count; r0 += 256, at += 256) {
+      int rows[8];
+      float v[8];
+      uint4 b[8], hi, mid, lo;
+      OuterRows<BITS8> x;
+#pragma unroll
+      for (int e = 0; e < 8; e++) rows[e] = list.rows[min(at, count - 1) + e];
+      x.load(a, rows, f < a.C ? f : 0);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = a.L[rows[e] * a.ldl + rank];
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = at + e < count ? v[e] : 0.0f;
+      x.operands(b, a.type);
+      split8(v, hi, mid, lo);
+#pragma unroll
+      for (int j = 0; j < 8; j++) {
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(b[j]), acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(mid), frag(b[j]), acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(b[j]), acc[j], 0, 0, 0);
+      }
+    }
+    if (wave * 32 < count)
+#pragma unroll
+      for (int j = 0; j < 8; j++) join[wave][j][lane] = acc[j];
+    __syncthreads();
+    // Wave w stores ranks w % 4 + 4 q, four of the lane's eight features
+    const int e = wave & 3, h = wave >> 2 << 2, r = rank0 + 4 * q + e;
+    if (f >= a.C || r >= R) return;
+    float* p = s.G + ((int64_t)n * R + r) * s.ldg + f + h;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int w = 0; w < 8 && w * 32 < count; w++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) sum[j] += ((const float*)&join[w][h + j][lane])[e];
+    sum *= s.scale;
+    if (accumulate) sum += *(const f32x4*)p;
+    *(f32x4*)p = sum;
+  }
+};
+__global__ void __launch_bounds__(512, 4)
+k_adapter_outer_few(AdapterSegments g, OuterArgs x, OuterArgs z, OuterSum gx, OuterSum gz, int R, int accumulate) {
+  __shared__ __align__(16) OuterFew few;
+  const bool second = (int)blockIdx.x >= x.fblocks;
+  const OuterArgs a = second ? z : x;
+  const OuterSum s = second ? gz : gx;
+  const int fb = second ? (int)blockIdx.x - x.fblocks : (int)blockIdx.x, rank0 = blockIdx.y * 16, n = blockIdx.z;
+  const int count = few.list.find(g, n);
+  if (count == 0 && accumulate) return;
+  if (a.type == M_BF16) few.run<false>(count, a, s, n, fb, rank0, R, accumulate);
+  else few.run<true>(count, a, s, n, fb, rank0, R, accumulate);
+}
+
 int mode(int dtype) { return dtype == SSTE_F8E4M3 ? M_E4M3 : dtype == SSTE_F8E5M2 ? M_E5M2 : dtype == SSTE_F8BLOCK ? M_BLOCK : M_BF16; }
 int padded_rank(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
 
@@ -809,6 +940,12 @@ void apply(const AdapterApply& a, hipStream_t s) {
   }
 }
 
+// One launch without chunks: its work grows with the adapters, for which the segments stand, and it reads M again for every 16 ranks.  Over 560 problems (64
+// to 2048 rows, 160 to 8192 features, ranks 16 to 128, 1 to 64 segments) the limit costs 0.8 % over the faster way in the mean, chunks everywhere 52 %.  64 rows
+// of 1280 + 5120, rank 64, nine segments: 5 us against 20; 2048 rows, one segment: 23 against 20.
+bool outer_few(int64_t T, int64_t segments, int R, int64_t I, int64_t O) {
+  return T <= kFewRows && segments <= kFewSegments && T * R * (I + O) * (segments > 8 ? segments : 8) <= 6000000000ll;
+}
 // Rows of a chunk of the weight gradients: about 384 workgroups of 256 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 44.4 us;
 // 256 workgroups 50.2, 512 46.7; 7777 ragged rows of 1280 + 5120, rank 64: 47.0, 52.1 and 54.2).  A chunk's sum has R / rows times four of its rows' bytes,
 // written and read again: where 384 give fewer than 4 R rows (rank 64, 4096 rows of 1280 + 1280: 19.6 us, with half of them 23.2), 4 R unless that leaves
@@ -841,16 +978,24 @@ size_t adapter_apply_workspace_bytes(int64_t T, int segments, int R, int64_t K, 
 }
 
 size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, int64_t O) {
-  if (T == 0) return 0;
+  if (T == 0 || outer_few(T, segments, R, I, O)) return 0;
   const AdapterSegments g = {nullptr, nullptr, segments, 0, (int)T};
   return (size_t)slots(g, outer_chunk(T, R, I, O)) * (size_t)R * (size_t)(I + O) * 4;
 }
 
 hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOuter& a, const AdapterOuter& b, int accumulate, void* ws, hipStream_t s) {
-  const int chunk = outer_chunk(g.T, R, a.C, b.C);
+  const bool few = outer_few(g.T, g.segments, R, a.C, b.C);
+  const int chunk = few ? 0 : outer_chunk(g.T, R, a.C, b.C), width = few ? 128 : 256;
   const auto args = [&](const AdapterOuter& o, float* part) {
-    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + 255) / 256, part};
+    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + width - 1) / width, part};
   };
+  if (few) {
+    const OuterArgs x = args(a, nullptr), z = args(b, nullptr);
+    const OuterSum gx = {nullptr, a.G, a.ldg, a.m_scale, a.C}, gz = {nullptr, b.G, b.ldg, b.m_scale, b.C};
+    const dim3 grid((unsigned)(x.fblocks + z.fblocks), (unsigned)((R + 15) / 16), (unsigned)g.adapters);
+    if (grid.x > 0 && grid.z > 0) SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_few, grid, dim3(512), s, g, x, z, gx, gz, R, accumulate);
+    return hipGetLastError();
+  }
   const OuterArgs x = args(a, (float*)ws), z = args(b, (float*)ws + slots(g, chunk) * R * a.C);
   if (g.T > 0 && x.fblocks + z.fblocks > 0) {
     const int64_t n = slots(g, chunk) * (x.fblocks + z.fblocks);

@@ -231,15 +231,16 @@ def test_rows_keep_to_themselves(sste, T):
     assert not torch.isfinite(Z1[hit].float()).any(dim=1).all() and not torch.isfinite(S1[hit]).any()
 
 
-def test_far_rows(sste):
+@pytest.mark.parametrize("T", [600, 2100])
+def test_far_rows(sste, T):
     """Row offsets beyond 2^32 bytes: a view of a large buffer with long rows."""
-    T, ld = 600, 1 << 22
+    ld = 1 << 22
     rng = np.random.default_rng(3)
-    room = torch.empty((T, ld), dtype=torch.bfloat16, device="cuda")              # 5 GB, read and written in its first columns only
+    room = torch.empty((T, ld), dtype=torch.bfloat16, device="cuda")              # 5 and 18 GB, read and written in its first columns only
     x, base = normal(rng, (T, 72), 1).to(torch.bfloat16), normal(rng, (T, 80), 1).to(torch.bfloat16)
     A, B = normal(rng, (2, 8, 72), 1).to(torch.bfloat16), normal(rng, (2, 8, 80), 1).to(torch.bfloat16)
     room[:, :72], room[:, 128:208] = x, base
-    seg = segments([0, 300, T], [1, 0])
+    seg = segments([0, T // 2, T], [1, 0])
     Z, S = sste.adapter_fwd(room[:, :72], *seg, A, B, base=room[:, 128:208], Z=room[:, 256:336])
     want = sste.adapter_fwd(x, *seg, A, B, base=base)
     assert torch.equal(Z, want[0]) and torch.equal(S, want[1])
@@ -293,20 +294,54 @@ def check_wgrad(sste, T, I, O, R, N, starts, ids, kind="bf16", x_kind="bf16", ac
     (95, 264, 512, 40, 2, [0, 63, 95], [1, 0]),                    # around the 64 rows of a step, and their halves
     (97, 256, 520, 72, 2, [0, 32, 97], [1, 0]),
     (2000, 136, 72, 96, 9, sorted(i * 7919 % 2001 for i in range(201)), [i % 10 for i in range(200)]),
+    (2047, 72, 264, 16, 2, [0, 100, 2040], [1, 0]),                # on both sides of the few rows that are one launch: rows
+    (2048, 264, 128, 40, 3, [0, 127, 128, 2048], [2, 1, 2]),
+    (2049, 136, 72, 40, 3, [0, 127, 128, 2049], [2, 1, 2]),
+    (511, 136, 72, 8, 3, [0, 255, 256, 511], [2, 1, 2]),
+    (513, 136, 72, 8, 3, [0, 1, 512, 513], [2, 1, 2]),
+    (256, 64, 136, 24, 5, list(range(257)), [i * 3 % 6 for i in range(256)]),                # segments
+    (256, 64, 136, 24, 5, [0] + list(range(257)), [i * 3 % 6 for i in range(257)]),
+    (256, 200, 16, 128, 1, sorted(i * 617 % 257 for i in range(257)), [0] * 256),
+    (250, 16, 200, 48, 3, sorted(i * 617 % 257 for i in range(257)), [i % 3 for i in range(256)]),
+    (70, 24, 40, 56, 2, [3, 3, 36, 36, 68], [0, 1, 0, 0]),
+    (2500, 392, 136, 64, 2, [10, 1200, 1280], [1, -1]),            # the same small sizes in chunks
+    (2100, 8, 264, 24, 2, [0, 1, 33], [1, 0]),
+    (2300, 136, 520, 16, 3, [0, 31], [2]),
 ])
 def test_wgrad(sste, T, I, O, R, N, starts, ids):
     check_wgrad(sste, T, I, O, R, N, starts, ids)
 
 
 @pytest.mark.parametrize("kind,x_kind", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e5m2", "checkpoint"), ("bf16", "checkpoint")])
-@pytest.mark.parametrize("R", [8, 32, 128])
-def test_wgrad_8_bit(sste, kind, x_kind, R):
-    check_wgrad(sste, 333, 208, 400, R, 3, [0, 100, 200, 320], [2, 0, 2], kind, x_kind)
+@pytest.mark.parametrize("R", [8, 32, 64, 128])
+@pytest.mark.parametrize("T", [333, 2333])
+def test_wgrad_8_bit(sste, kind, x_kind, R, T):
+    check_wgrad(sste, T, 208, 400, R, 3, [0, 100, 200, T - 13], [2, 0, 2], kind, x_kind)
 
 
 @pytest.mark.parametrize("accumulate,pad", [(True, 0), (True, 16), (False, 16)])
-def test_wgrad_accumulates_and_strides(sste, accumulate, pad):
-    check_wgrad(sste, 500, 144, 272, 16, 3, [0, 100, 500], [2, 0], accumulate=accumulate, pad=pad)
+@pytest.mark.parametrize("T", [500, 2500])
+def test_wgrad_accumulates_and_strides(sste, accumulate, pad, T):
+    check_wgrad(sste, T, 144, 272, 16, 3, [0, 100, T], [2, 0], accumulate=accumulate, pad=pad)
+
+
+@pytest.mark.parametrize("T", [100, 2300])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_wgrad_keeps_to_its_rows(sste, T, kind):
+    """NaN in the rows of one adapter, of none and of no segment reach no other adapter's gradients."""
+    rng = np.random.default_rng(6)
+    X, _, dt, xs = stored(sste, normal(rng, (T, 144), 1), kind)
+    dZ, S, dS = normal(rng, (T, 80), 1).to(torch.bfloat16), normal(rng, (T, 40), 1), normal(rng, (T, 40), 1)
+    seg = segments([5, 17, 40, 66, T - 20], [1, 0, -1, 2])
+    want = sste.adapter_wgrad(dZ, X, S, dS, *seg, 3, x_dtype=dt, x_scale=xs)
+    for part in (slice(0, 17), slice(40, 66), slice(T - 20, T)):
+        for t in (dZ, S, dS):
+            t[part] = float("nan")
+        X[part] = float("nan") if kind == "bf16" else 0x7F
+    dA, dB = sste.adapter_wgrad(dZ, X, S, dS, *seg, 3, x_dtype=dt, x_scale=xs)
+    for n in (0, 2):
+        assert torch.equal(dA[n], want[0][n]) and torch.equal(dB[n], want[1][n])
+    assert dA[1].isnan().all() and dB[1].isnan().all()
 
 
 def test_wgrad_empty(sste):
@@ -381,7 +416,8 @@ def test_native_marshalling(sste):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: sste.adapter_fwd(X, *seg, A[:, :, :], B, dtype=9), lambda: sste.checkpoint_backward(codes, blocks, act=7),
-                 lambda: sste.adapter_wgrad(dZ, X, S, S, *seg, N, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
+                 lambda: sste.adapter_wgrad(*(torch.zeros((4000, t.shape[1]), dtype=t.dtype, device="cuda") for t in (dZ, X, S, S)), *seg, N,
+                                            workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(sste.SsteError):
             call()
 
