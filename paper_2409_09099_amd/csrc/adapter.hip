@@ -8,6 +8,8 @@
 // exchanged, and the two weight gradients are one.  The rank is small: all three are bound by the bytes of X, base, out and M.
 #include "adapter.h"
 
+#include <cmath>
+
 namespace sste {
 
 namespace {
@@ -872,19 +874,28 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   const int64_t extra = (g.segments < g.T ? g.segments : g.T) + 1;     // tiles that segments, and the rows outside them, may add
   const int rank = padded_rank(R);
   int chunk = down_chunk(rank, 16), chunks = K > 0 ? (K + chunk - 1) / chunk : 1;
-  // One launch saves one, about 3 us, and does the first product in 16-row tiles without sharing its contraction out.  Rank 16, 1280 -> 3840: 1 row 5.6
-  // against 8.6, 1024 rows 9.2 against 11.2; rank 64, 1280 -> 5120: 512 rows 11.7 against 12.3, 1024 rows 16.7 against 14.9; rank 16, 5120 -> 1280 (20
-  // chunks): 64 rows of two segments 8.5 against 9.1, 256 rows of four 11.6 against 9.2, 256 rows of as many 12.7 against 16.5.
-  const bool single = 2 * (int64_t)g.segments >= g.T;                  // mostly one row a segment: tiles are as good as empty whatever their size
-  p.both = (int64_t)g.T * chunks <= 5120 && (chunks <= 10 || g.T <= 64 || single);
-  const int64_t all = g.T / (p.both ? 16 : 32) + extra;
+  // One launch does the first product in 16-row tiles, once for each of a tile's workgroups, and cannot share its contraction out.  Its time against that of
+  // two, in us: the chunks' and the features' latencies by rounds of workgroups, and what does not come from the last-level cache, against rows and adapters by
+  // bytes.  The factors are fitted to 2648 problems (ranks 16 to 128, 112 ... 5120 -> 136 ... 5120, 8 ... 32768 rows, up to a segment each): the choice costs
+  // 0.75 % over the better in the mean, where limits on rows and chunks cost 5 % and 87 % at most.  Rank 16, 1280 -> 3840: 1 row 5.6 against 8.6; rank 64,
+  // 512 -> 208, 2500 rows 5.6 against 8.4; rank 64, 5120 -> 1280, 64 rows 16.6 against 10.7; rank 16, 1280 -> 5120, 1000 rows of their own 28.8 against 53.9,
+  // 32768 rows of one segment 178 against 146 (rank 32).
+  const bool single = 2 * (int64_t)g.segments >= g.T;                  // mostly one row a segment: a tile is as good as empty, whatever its size
+  const int64_t passes = C > 0 ? (C + 1023) / 1024 : 1, tiles16 = g.T / 16 + extra, most = (1 << 22) / (slots(g, 16) + 8);
+  int64_t slices = 520 / tiles16 < passes ? 520 / tiles16 : passes;
+  if (slices > most) slices = most;                                    // what a grid can count, with a million empty segments
+  if (slices < 1) slices = 1;
+  const double r = rank / 64.0, few = extra - 1;
+  const auto filled = [&](int rows) { return fmax(few, (double)g.T / rows + few * 0.5); };      // tiles with rows, more or less
+  const double at_once = 200 * (single ? 1 + 8.0 / rank : 1) / (rank == 128 ? 1.5 : 1), mb = 1e-6 * g.T * (2.0 * K + 4.0 * C);
+  const double one = 2 + (0.23 * chunks * (1 + r) + 0.8 * passes / slices * (1 + 1.8 * r)) * fmax(1, filled(16) * slices / at_once) + 0.1 * fmax(0, mb - 90);
+  const double two = 7.8 + 1.1 * r + 0.14 * K / 1280.0 * (1 + r) + 0.085 * mb + 0.24e-6 * filled(32) * rank * ((double)K + C);
+  p.both = one <= two && most > 0;
+  const int64_t all = p.both ? tiles16 : g.T / 32 + extra;
   if (p.both) {
     // A tile's workgroups read the same rows and the same adapter: on one XCD (rank 16, 2560 -> 2560, 200 rows of 6 segments 6.0 us against 7.9; 96 of 96, 1280
     // -> 3840, 8.2 against 8.7, though -> 5120 9.9 against 9.2), unless some XCDs would have no tile (rank 128, 1280 -> 5120, 1 row: 13.1 against 10.7).
-    const int64_t passes = C > 0 ? (C + 1023) / 1024 : 1, most = (1 << 22) / (slots(g, 16) + 8);      // what a grid can count, with a million empty segments
-    int64_t slices = 520 / all < passes ? 520 / all : passes;
-    if (slices > most) slices = most;
-    p.share = share_of((int)(slices < 1 ? 1 : slices), all >= 8);
+    p.share = share_of((int)slices, all >= 8);
     return p;
   }
   // Tiles of 32 or 64 rows, which read the adapter half as often (not of rank 16, whose adapters are small: 16384 rows of 4096 48.7 us against 57), and the

@@ -98,7 +98,7 @@ def test_bf16(sste, shape, fwd):
     check_apply(sste, fwd, *shape, "bf16")
 
 
-@pytest.mark.parametrize("T,K,C,R", [(1, 16, 8, 8), (19, 144, 520, 16), (130, 1296, 136, 48), (65, 592, 264, 128)])
+@pytest.mark.parametrize("T,K,C,R", [(1, 16, 8, 8), (19, 144, 520, 16), (130, 1296, 136, 48), (65, 592, 264, 128), (700, 2064, 136, 64), (3000, 5120, 1032, 16), (3000, 5120, 1032, 32)])
 @pytest.mark.parametrize("fwd,kind", [(True, "e4m3"), (False, "e4m3"), (False, "e5m2")])
 def test_8_bit(sste, T, K, C, R, fwd, kind):
     check_apply(sste, fwd, T, K, C, R, 3, [0, T // 2, T], [2, 0], kind)
@@ -106,19 +106,16 @@ def test_8_bit(sste, T, K, C, R, fwd, kind):
 
 @pytest.mark.parametrize("R", [8, 16, 24, 32, 64, 128])
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
-@pytest.mark.parametrize("K", [208, 2064])
-def test_long_batches(sste, R, kind, K):
-    """Many rows, in tiles of 32 and (long contractions) of 64, ragged segments among them."""
-    T = 8300
-    check_apply(sste, True, T, K, 264, R, 3, [5, 70, 134, 199, 8200], [2, -1, 0, 1], kind, seed=R)
+@pytest.mark.parametrize("T,K,C", [(8300, 208, 264), (4300, 2064, 264), (3100, 5120, 1032)])
+def test_long_batches(sste, R, kind, T, K, C):
+    """Many rows, in tiles of 16, 32 and (long contractions) of 64, ragged segments among them."""
+    check_apply(sste, True, T, K, C, R, 3, [5, 70, 134, 199, T - 100], [2, -1, 0, 1], kind, seed=R)
 
 
-@pytest.mark.parametrize("R", [8, 32, 64, 128])
-@pytest.mark.parametrize("K", [2056, 5120])
+@pytest.mark.parametrize("T,K,C,R", [(3000, 5120, 1032, 8), (3000, 5120, 1032, 32), (700, 2056, 136, 64), (700, 5120, 136, 64), (700, 2056, 136, 128), (700, 5120, 136, 128)])
 @pytest.mark.parametrize("fwd", [True, False])
-def test_split_contraction(sste, R, K, fwd):
+def test_split_contraction(sste, T, K, C, R, fwd):
     """The first product shared out among workgroups, into a workspace; without one, or with one that is too small, not shared out."""
-    T, C = 700, 136
     need = sste.adapter_workspace_bytes(T, 3, R, K, C)
     assert need > 0 and need % (T * R * 4) == 0
     for workspace in (None, torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(need - 1, dtype=torch.uint8, device="cuda"),
@@ -127,9 +124,9 @@ def test_split_contraction(sste, R, K, fwd):
 
 
 @pytest.mark.parametrize("base,scale,in_place,pad", [(False, True, False, 0), (True, False, False, 16), (True, True, True, 16), (False, False, False, 0), (True, True, True, 0)])
-@pytest.mark.parametrize("T", [37, 8200])
-def test_base_scale_strides(sste, base, scale, in_place, pad, T):
-    check_apply(sste, True, T, 144, 136, 16, 3, [0, 9, 20, T - 4], [1, -1, 2], "bf16", base, scale, in_place, pad)
+@pytest.mark.parametrize("T,K,C,R", [(37, 144, 136, 16), (8200, 144, 136, 16), (3000, 5120, 1032, 16), (700, 2056, 136, 64), (5000, 2056, 136, 128)])
+def test_base_scale_strides(sste, base, scale, in_place, pad, T, K, C, R):
+    check_apply(sste, True, T, K, C, R, 3, [0, 9, 20, T - 4], [1, -1, 2], "bf16", base, scale, in_place, pad)
 
 
 @pytest.mark.parametrize("S", [63, 64, 65, 200, 4100, 5000])
@@ -141,8 +138,8 @@ def test_many_segments(sste, S):
     check_apply(sste, True, T, 64, 64, 8, 9, starts, rng.integers(-1, 9, S).tolist(), "bf16")
 
 
-@pytest.mark.parametrize("T,K,R", [(511, 1280, 16), (512, 1280, 64), (513, 1280, 64), (1024, 1280, 16), (1025, 1280, 16), (64, 5120, 16), (65, 5120, 16), (320, 1024, 128), (647, 1024, 128),
-                                   (8191, 2056, 64), (8192, 2056, 64), (5003, 2056, 128)])
+@pytest.mark.parametrize("T,K,R", [(74, 5120, 16), (75, 5120, 16), (6003, 1280, 64), (6004, 1280, 64), (621, 1024, 128), (622, 1024, 128), (2787, 1024, 128), (2788, 1024, 128), (1848, 2056, 64),
+                                   (1849, 2056, 64), (4324, 2056, 64), (4325, 2056, 64), (5003, 2056, 128), (8192, 2056, 128)])
 def test_around_the_plans_ends(sste, T, K, R):
     """Sizes on both sides of every choice between the ways of sharing the products out."""
     check_apply(sste, True, T, K, 136, R, 2, [0, T // 3, T], [1, 0], "bf16")
@@ -150,16 +147,16 @@ def test_around_the_plans_ends(sste, T, K, R):
 
 def test_a_million_empty_segments(sste):
     S = 1 << 20
-    for K in (64, 2816):                                                                # in one launch and in two
-        check_apply(sste, True, 1 if K == 64 else 70, K, 7168, 8, 2, [0] * S + [1], [0] * (S - 1) + [1], "bf16")
+    for T, K, R in ((1, 64, 8), (70, 5120, 64)):                                        # in one launch and in two
+        check_apply(sste, True, T, K, 7168, R, 2, [0] * S + [1], [0] * (S - 1) + [1], "bf16")
 
 
-@pytest.mark.parametrize("T", [9, 8200])
-def test_empty(sste, T):
+@pytest.mark.parametrize("T,I,O,R", [(9, 64, 72, 8), (8200, 64, 72, 8), (700, 2056, 136, 64)])          # in one launch, and in two with a shared contraction
+def test_empty(sste, T, I, O, R):
     """No rows, no segments, no adapters, no columns."""
     rng = np.random.default_rng(0)
-    X, A, B = normal(rng, (T, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 72), 1).to(torch.bfloat16)
-    base = normal(rng, (T, 72), 1).to(torch.bfloat16)
+    X, A, B = normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (2, R, I), 1).to(torch.bfloat16), normal(rng, (2, R, O), 1).to(torch.bfloat16)
+    base = normal(rng, (T, O), 1).to(torch.bfloat16)
     rs, sa = segments([0], [])
     Z, S = sste.adapter_fwd(X, rs, sa, A, B, base=base)
     assert torch.equal(Z, base) and not S.any()
@@ -167,7 +164,7 @@ def test_empty(sste, T):
     Z, S = sste.adapter_fwd(X, rs, sa, A[:0], B[:0], base=base)
     assert torch.equal(Z, base) and not S.any()
     Z, S = sste.adapter_fwd(X[:0], rs, sa, A, B)
-    assert Z.shape == (0, 72) and S.shape == (0, 8)
+    assert Z.shape == (0, O) and S.shape == (0, R)
     Z, S = sste.adapter_fwd(X[:, :0], rs, sa, A[:, :, :0], B, base=base)
     assert torch.equal(Z, base) and not S.any()
     Z, S = sste.adapter_fwd(X, rs, sa, A, B[:, :, :0])
@@ -175,37 +172,37 @@ def test_empty(sste, T):
     within("S", S, want[1], want[2])
 
 
-@pytest.mark.parametrize("T", [5, 8200])
-def test_no_segments_need_no_arrays(sste, T):
+@pytest.mark.parametrize("T,I,O,R", [(5, 64, 72, 8), (8200, 64, 72, 8), (700, 2056, 136, 64)])
+def test_no_segments_need_no_arrays(sste, T, I, O, R):
     """segments = 0 through the C ABI, with NULL for both arrays."""
     rng = np.random.default_rng(4)
-    X, base = normal(rng, (T, 64), 1).to(torch.bfloat16), normal(rng, (T, 72), 1).to(torch.bfloat16)
-    A, B = normal(rng, (2, 8, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 72), 1).to(torch.bfloat16)
-    Z, S = torch.full_like(base, 7), torch.full((T, 8), 7.0, device="cuda")
-    dA, dB = torch.full((2, 8, 64), 7.0, device="cuda"), torch.full((2, 8, 72), 7.0, device="cuda")
-    ws = torch.empty(sste.adapter_wgrad_workspace_bytes(T, 0, 8, 64, 72), dtype=torch.uint8, device="cuda")
+    X, base = normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (T, O), 1).to(torch.bfloat16)
+    A, B = normal(rng, (2, R, I), 1).to(torch.bfloat16), normal(rng, (2, R, O), 1).to(torch.bfloat16)
+    Z, S = torch.full_like(base, 7), torch.full((T, R), 7.0, device="cuda")
+    dA, dB = torch.full((2, R, I), 7.0, device="cuda"), torch.full((2, R, O), 7.0, device="cuda")
+    ws = torch.empty(sste.adapter_wgrad_workspace_bytes(T, 0, R, I, O), dtype=torch.uint8, device="cuda")
     lib, p, stream = sste.library(), lambda t: t.data_ptr(), torch.cuda.current_stream().cuda_stream      # noqa: E731
-    assert lib.sste_adapter_fwd(p(X), T, 64, 64, 0, 1.0, None, 0, None, p(A), 64, p(B), 72, None, 2, 8, 72, p(base), 72, p(Z), 72, p(S), 8, None, 0, stream) == 0
-    assert lib.sste_adapter_wgrad(p(base), T, 72, 72, 0, 1.0, p(X), 64, 64, 0, 1.0, None, 0, p(S), 8, p(S), 8, None, 0, None, 2, 8, p(dA), 64, p(dB), 72, 0, p(ws), ws.numel(), stream) == 0
+    assert lib.sste_adapter_fwd(p(X), T, I, I, 0, 1.0, None, 0, None, p(A), I, p(B), O, None, 2, R, O, p(base), O, p(Z), O, p(S), R, None, 0, stream) == 0
+    assert lib.sste_adapter_wgrad(p(base), T, O, O, 0, 1.0, p(X), I, I, 0, 1.0, None, 0, p(S), R, p(S), R, None, 0, None, 2, R, p(dA), I, p(dB), O, 0, p(ws), ws.numel(), stream) == 0
     assert torch.equal(Z, base) and not S.any() and not dA.any() and not dB.any()
 
 
-@pytest.mark.parametrize("T", [40, 8200])
-def test_malformed_segments_stay_inside(sste, T):
+@pytest.mark.parametrize("T,I,O,R", [(40, 64, 72, 8), (8200, 64, 72, 8), (700, 2056, 136, 64)])
+def test_malformed_segments_stay_inside(sste, T, I, O, R):
     """Bounds beyond the rows are clamped, and bounds that decrease leave the memory around the outputs alone."""
     rng = np.random.default_rng(1)
-    X, A, B = normal(rng, (T, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 64), 1).to(torch.bfloat16), normal(rng, (2, 8, 72), 1).to(torch.bfloat16)
-    room_z = torch.full((T + 32, 80), 7.0, dtype=torch.bfloat16, device="cuda")
-    room_s = torch.full((T + 32, 12), 7.0, dtype=torch.float32, device="cuda")
-    Z, S = room_z[16:-16, :72], room_s[16:-16, :8]
+    X, A, B = normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (2, R, I), 1).to(torch.bfloat16), normal(rng, (2, R, O), 1).to(torch.bfloat16)
+    room_z = torch.full((T + 32, O + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    room_s = torch.full((T + 32, R + 4), 7.0, dtype=torch.float32, device="cuda")
+    Z, S = room_z[16:-16, :O], room_s[16:-16, :R]
     for starts, ids in (([-5, 20, T + 100], [0, 1]), ([30, 10, T], [0, 1]), ([2 ** 31 - 1, -2 ** 31, 5, 2 ** 31 - 1], [0, 1, 0])):
         rs, sa = segments(starts, ids)
         sste.adapter_fwd(X, rs, sa, A, B, Z=Z, S=S)
         torch.cuda.synchronize()
-        for room, w in ((room_z, 72), (room_s, 8)):
+        for room, w in ((room_z, O), (room_s, R)):
             assert (room[:16] == 7).all() and (room[-16:] == 7).all() and (room[:, w:] == 7).all()
-        need = sste.adapter_wgrad_workspace_bytes(T, len(ids), 8, 64, 72)
-        ws, room_g = torch.full((need + 256,), 0x11, dtype=torch.uint8, device="cuda"), torch.full((4, 8, 64), 7.0, device="cuda")
+        need = sste.adapter_wgrad_workspace_bytes(T, len(ids), R, I, O)
+        ws, room_g = torch.full((need + 256,), 0x11, dtype=torch.uint8, device="cuda"), torch.full((4, R, I), 7.0, device="cuda")
         sste.adapter_wgrad(Z, X, S, S, rs, sa, 2, dA=room_g[1:3], workspace=ws[:need])
         assert (ws[need:] == 0x11).all() and (room_g[0] == 7).all() and (room_g[3] == 7).all()
     rs, sa = segments([-5, 20, T + 100], [0, 1])
@@ -213,11 +210,11 @@ def test_malformed_segments_stay_inside(sste, T):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-@pytest.mark.parametrize("T", [40, 8200])
-def test_rows_keep_to_themselves(sste, T):
+@pytest.mark.parametrize("T,I,O,R", [(40, 128, 136, 16), (8200, 128, 136, 16), (700, 2056, 136, 64)])
+def test_rows_keep_to_themselves(sste, T, I, O, R):
     """A row's infinities and NaN reach no other row, an adapter's no row of another adapter; a row's result does not depend on the other rows."""
     rng = np.random.default_rng(2)
-    X, A, B = normal(rng, (T, 128), 1).to(torch.bfloat16), normal(rng, (3, 16, 128), 1).to(torch.bfloat16), normal(rng, (3, 16, 136), 1).to(torch.bfloat16)
+    X, A, B = normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (3, R, I), 1).to(torch.bfloat16), normal(rng, (3, R, O), 1).to(torch.bfloat16)
     seg = segments([0, 10, 21, T], [0, 1, 0])
     Z0, S0 = sste.adapter_fwd(X, *seg, A, B)
     X2, A2 = X.clone(), A.clone()
@@ -451,7 +448,7 @@ def test_gradients_against_differences(sste):
             assert abs((up - down) - g[at]) <= step * np.abs(g).max() + 1e-9 * abs(up), (name, at)
 
 
-@pytest.mark.parametrize("T,I,O,R", [(300, 136, 264, 16), (2500, 2056, 520, 64)])          # one launch a product; shared out, with workspaces of the graph's own
+@pytest.mark.parametrize("T,I,O,R", [(300, 136, 264, 16), (700, 2056, 520, 64), (2500, 2056, 520, 128)])          # one launch a product; shared out, with workspaces of the graph's own
 def test_other_stream_and_graph(sste, T, I, O, R):
     """Captured once, replayed with other segments, adapters and rows written into the same tensors, between eager work."""
     rng = np.random.default_rng(11)
@@ -494,7 +491,7 @@ def test_other_stream_and_graph(sste, T, I, O, R):
 def test_two_streams_at_once(sste):
     """Two batches on two streams, each with its own workspaces and outputs, the same adapters: as one after the other."""
     rng = np.random.default_rng(29)
-    T, I, O, R, N = 2500, 2056, 520, 32, 3
+    T, I, O, R, N = 2500, 2056, 520, 128, 3
     A, B = normal(rng, (N, R, I), 0.1).to(torch.bfloat16), normal(rng, (N, R, O), 0.1).to(torch.bfloat16)
     batches = [(normal(rng, (T, I), 1).to(torch.bfloat16), normal(rng, (T, O), 1).to(torch.bfloat16), *segments([0, n, T - 9], [2, k])) for n, k in ((700, 0), (33, 2))]
 
