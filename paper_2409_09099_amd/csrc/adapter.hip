@@ -747,7 +747,8 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
 // Both weight gradients of few rows in one launch: a workgroup takes 128 features of one adapter, 16 ranks, and all rows that the adapter has, 32 in each of
 // eight waves at a time.  The rows are listed in LDS first, in order, by a search of every row's segment, so that an adapter's short segments share a step; behind the
 // last the list repeats it, with zeros of L.  The waves' sums meet in LDS, in the order of the rows.
-// Bound by the launch and the waits in a row: the bounds, the rows of L and M, the stores.
+// Bound by the launch and the waits in a row: the bounds, the rows of L and M, the stores (4 rows of 80 + 80, rank 16: 3.8 us; 256 rows of 1280 + 5120, rank
+// 128, of one adapter 7.1, of seven 20).
 constexpr int kFewRows = 2048, kFewSegments = 256;
 struct RowList {
   int start[kFewSegments + 1], adapter[kFewSegments], counts[kFewRows / 64];
@@ -877,7 +878,7 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   // One launch does the first product in 16-row tiles, once for each of a tile's workgroups, and cannot share its contraction out.  Its time against that of
   // two, in us: the chunks' and the features' latencies by rounds of workgroups, and what does not come from the last-level cache, against rows and adapters by
   // bytes.  The factors are fitted to 2648 problems (ranks 16 to 128, 112 ... 5120 -> 136 ... 5120, 8 ... 32768 rows, up to a segment each): the choice costs
-  // 0.75 % over the better in the mean, where limits on rows and chunks cost 5 % and 87 % at most.  Rank 16, 1280 -> 3840: 1 row 5.6 against 8.6; rank 64,
+  // 0.75 % over the better in the mean and 70 % at most, where limits on rows and chunks cost 5 % and 87 %.  Rank 16, 1280 -> 3840: 1 row 5.6 against 8.6; rank 64,
   // 512 -> 208, 2500 rows 5.6 against 8.4; rank 64, 5120 -> 1280, 64 rows 16.6 against 10.7; rank 16, 1280 -> 5120, 1000 rows of their own 28.8 against 53.9,
   // 32768 rows of one segment 178 against 146 (rank 32).
   const bool single = 2 * (int64_t)g.segments >= g.T;                  // mostly one row a segment: a tile is as good as empty, whatever its size
