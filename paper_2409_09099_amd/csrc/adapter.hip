@@ -705,27 +705,34 @@ struct OuterSum {
   float scale;
   int C;
 };
-// Adds the chunks of adapter n in the order of their rows.  Bound by the reads, which mostly come from the last-level cache (34 MB in 9 us).
+// Adds the chunks of adapter n in a fixed order.  Bound by the reads, which mostly come from the last-level cache (34 MB in 9 us), and where there are few
+// features, ranks and adapters by the waits for eight chunks after eight: then (`shares` 4, otherwise 1) a workgroup's waves take eight of them each in turn
+// for the same 256 features, and meet in LDS.  Both kernels, 8192 rows of 80 + 80, rank 16: 9.8 us against 22.2; but 3000 rows of 1280 + 5120, rank 128,
+// seven adapters 74 against 49.
 __global__ void __launch_bounds__(256)
-k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b, int ablocks, int accumulate) {
+k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b, int ablocks, int shares, int accumulate) {
   const bool second = (int)blockIdx.x >= ablocks;
   const OuterSum s = second ? b : a;
-  const int f = ((int)(second ? blockIdx.x - ablocks : blockIdx.x) * 256 + (int)threadIdx.x) * 4, r = blockIdx.y, n = blockIdx.z;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int block = second ? (int)blockIdx.x - ablocks : (int)blockIdx.x, f = ((shares > 1 ? block : block * 4 + wave) * 64 + lane) * 4, r = blockIdx.y, n = blockIdx.z;
   const bool in = f < s.C;                             // the lanes stay together for the segments
+  __shared__ f32x4 join[3][64];
   f32x4 sum = {0, 0, 0, 0};
+  int turn = 0;
   const float* from = s.part + (int64_t)r * s.C + f;
   const int64_t stride = (int64_t)R * s.C;
   // 64 segments at a time: each lane looks at one, and those of adapter n are worked through in order
   for (int v0 = 1; v0 <= g.segments; v0 += 64) {
-    const int v = v0 + ((int)threadIdx.x & 63);
+    const int v = v0 + lane;
     const int rows = segment_bound(g, v + 1) - segment_bound(g, v), first = first_slot(g, v, chunk);
     const int last = min(first + (rows - 1) / chunk + 1, first_slot(g, v + 1, chunk));
     uint64_t todo = __ballot(v <= g.segments && rows > 0 && segment_adapter(g, v) == n);
     while (todo) {
-      const int lane = __builtin_ctzll(todo);
+      const int of = __builtin_ctzll(todo);
       todo &= todo - 1;
-      const int end = __builtin_amdgcn_readlane(last, lane);
-      for (int k = __builtin_amdgcn_readlane(first, lane); k < end; k += 8) {
+      const int end = __builtin_amdgcn_readlane(last, of);
+      for (int k = __builtin_amdgcn_readlane(first, of); k < end; k += 8, turn++) {
+        if (shares > 1 && (turn & 3) != wave) continue;
         f32x4 part[8];                                 // all under way at once
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -736,6 +743,13 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
         for (int i = 0; i < 8; i++) sum += part[i];
       }
     }
+  }
+  if (shares > 1) {
+    if (wave > 0) join[wave - 1][lane] = sum;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; w++) sum += join[w][lane];
   }
   if (!in) return;
   float* p = s.G + ((int64_t)n * R + r) * s.ldg + f;
@@ -961,12 +975,15 @@ bool outer_few(int64_t T, int64_t segments, int R, int64_t I, int64_t O) {
 // Rows of a chunk of the weight gradients: about 384 workgroups of 256 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 44.4 us;
 // 256 workgroups 50.2, 512 46.7; 7777 ragged rows of 1280 + 5120, rank 64: 47.0, 52.1 and 54.2).  A chunk's sum has R / rows times four of its rows' bytes,
 // written and read again: where 384 give fewer than 4 R rows (rank 64, 4096 rows of 1280 + 1280: 19.6 us, with half of them 23.2), 4 R unless that leaves
-// fewer than 256 workgroups.
+// fewer than 256 workgroups.  Narrow layers have few workgroups however short the chunks, and the waits for 64 rows in a chunk and for eight chunks in a sum
+// balance at a chunk of 64 sqrt(T / 950) rows (over 576 problems of 3000 ... 16384 rows 1.2 % in the mean, 8192 rows of 80 + 80 up to 20 %).
 int outer_chunk(int64_t T, int R, int64_t I, int64_t O) {
   const int64_t blocks = ((I + 255) / 256 + (O + 255) / 256) * (R > 64 ? 2 : 1), least = 4 * padded_rank(R), most = 1 << 20;
   const auto rows = [&](int64_t workgroups) { return (T * blocks / workgroups + 63) / 64 * 64; };
+  const int64_t shortest = (int64_t)sqrt(T / 950.0) * 64;
   int64_t chunk = rows(384);
   if (chunk < least) chunk = rows(256) < least ? rows(256) : least;
+  if (chunk < shortest) chunk = shortest;
   return (int)(chunk < 64 ? 64 : chunk > most ? most : chunk);
 }
 
@@ -997,9 +1014,9 @@ size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, 
 
 hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOuter& a, const AdapterOuter& b, int accumulate, void* ws, hipStream_t s) {
   const bool few = outer_few(g.T, g.segments, R, a.C, b.C);
-  const int chunk = few ? 0 : outer_chunk(g.T, R, a.C, b.C), width = few ? 128 : 256;
+  const int chunk = few ? 0 : outer_chunk(g.T, R, a.C, b.C), span = few ? 128 : 256;
   const auto args = [&](const AdapterOuter& o, float* part) {
-    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + width - 1) / width, part};
+    return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + span - 1) / span, part};
   };
   if (few) {
     const OuterArgs x = args(a, nullptr), z = args(b, nullptr);
@@ -1018,10 +1035,12 @@ hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOu
       default: SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer<4>, grid, dim3(256), s, g, x, z, R, chunk); break;
     }
   }
-  const int ablocks = (a.C + 1023) / 1024, bblocks = (b.C + 1023) / 1024;
+  // Chunks shared out among a workgroup's waves while that gives no more than 2048 workgroups, and where an adapter has more than eight in the mean
+  const int64_t wide = (int64_t)((a.C + 1023) / 1024 + (b.C + 1023) / 1024) * R * g.adapters;
+  const int shares = wide <= 512 && slots(g, chunk) > 8 * (int64_t)g.adapters ? 4 : 1, width = 1024 / shares, ablocks = (a.C + width - 1) / width, bblocks = (b.C + width - 1) / width;
   if (ablocks + bblocks > 0 && g.adapters > 0)
     SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_sum, dim3((unsigned)(ablocks + bblocks), (unsigned)R, (unsigned)g.adapters), dim3(256), s, g, R, chunk,
-                (OuterSum{x.part, a.G, a.ldg, a.m_scale, a.C}), (OuterSum{z.part, b.G, b.ldg, b.m_scale, b.C}), ablocks, accumulate);
+                (OuterSum{x.part, a.G, a.ldg, a.m_scale, a.C}), (OuterSum{z.part, b.G, b.ldg, b.m_scale, b.C}), ablocks, shares, accumulate);
   return hipGetLastError();
 }
 
