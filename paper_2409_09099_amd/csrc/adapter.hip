@@ -714,48 +714,58 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
   const bool second = (int)blockIdx.x >= ablocks;
   const OuterSum s = second ? b : a;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int block = second ? (int)blockIdx.x - ablocks : (int)blockIdx.x, f = ((shares > 1 ? block : block * 4 + wave) * 64 + lane) * 4, r = blockIdx.y, n = blockIdx.z;
+  const int block = second ? (int)blockIdx.x - ablocks : (int)blockIdx.x, f = ((shares > 1 ? block : block * 4 + wave) * 64 + lane) * 4, n = blockIdx.z;
   const bool in = f < s.C;                             // the lanes stay together for the segments
   __shared__ f32x4 join[3][64];
-  f32x4 sum = {0, 0, 0, 0};
-  int turn = 0;
-  const float* from = s.part + (int64_t)r * s.C + f;
-  const int64_t stride = (int64_t)R * s.C;
-  // 64 segments at a time: each lane looks at one, and those of adapter n are worked through in order
-  for (int v0 = 1; v0 <= g.segments; v0 += 64) {
-    const int v = v0 + lane;
-    const int rows = segment_bound(g, v + 1) - segment_bound(g, v), first = first_slot(g, v, chunk);
-    const int last = min(first + (rows - 1) / chunk + 1, first_slot(g, v + 1, chunk));
-    uint64_t todo = __ballot(v <= g.segments && rows > 0 && segment_adapter(g, v) == n);
-    while (todo) {
-      const int of = __builtin_ctzll(todo);
-      todo &= todo - 1;
-      const int end = __builtin_amdgcn_readlane(last, of);
-      for (int k = __builtin_amdgcn_readlane(first, of); k < end; k += 8, turn++) {
-        if (shares > 1 && (turn & 3) != wave) continue;
-        f32x4 part[8];                                 // all under way at once
+  for (int r = blockIdx.y; r < R; r += gridDim.y) {
+    f32x4 sum = {0, 0, 0, 0};
+    int turn = 0;
+    bool rows_of_it = false;
+    const float* from = s.part + (int64_t)r * s.C + f;
+    const int64_t stride = (int64_t)R * s.C;
+    // 64 segments at a time: each lane looks at one, and those of adapter n are worked through in order
+    for (int v0 = 1; v0 <= g.segments; v0 += 64) {
+      const int v = v0 + lane;
+      const int rows = segment_bound(g, v + 1) - segment_bound(g, v), first = first_slot(g, v, chunk);
+      const int last = min(first + (rows - 1) / chunk + 1, first_slot(g, v + 1, chunk));
+      uint64_t todo = __ballot(v <= g.segments && rows > 0 && segment_adapter(g, v) == n);
+      rows_of_it |= todo != 0;
+      while (todo) {
+        const int of = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int end = __builtin_amdgcn_readlane(last, of);
+        for (int k = __builtin_amdgcn_readlane(first, of); k < end; k += 8, turn++) {
+          if (shares > 1 && (turn & 3) != wave) continue;
+          f32x4 part[8];                                 // all under way at once
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          part[i] = (f32x4){0, 0, 0, 0};
-          if (in && k + i < end) part[i] = *(const f32x4*)(from + (k + i) * stride);
+          for (int i = 0; i < 8; i++) {
+            part[i] = (f32x4){0, 0, 0, 0};
+            if (in && k + i < end) part[i] = *(const f32x4*)(from + (k + i) * stride);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; i++) sum += part[i];
         }
-#pragma unroll
-        for (int i = 0; i < 8; i++) sum += part[i];
       }
     }
-  }
-  if (shares > 1) {
-    if (wave > 0) join[wave - 1][lane] = sum;
-    __syncthreads();
-    if (wave > 0) return;
+    if (!rows_of_it) {                                   // nothing to add, in any rank: zeros, or as it is
+      if (!accumulate && in && (shares == 1 || wave == 0))
+        for (; r < R; r += gridDim.y) *(f32x4*)(s.G + ((int64_t)n * R + r) * s.ldg + f) = (f32x4){0, 0, 0, 0};
+      return;
+    }
+    if (shares > 1) {
+      if (wave > 0) join[wave - 1][lane] = sum;
+      __syncthreads();
+      if (wave == 0)
 #pragma unroll
-    for (int w = 0; w < 3; w++) sum += join[w][lane];
+        for (int w = 0; w < 3; w++) sum += join[w][lane];
+      __syncthreads();
+    }
+    if (!in || (shares > 1 && wave > 0)) continue;
+    float* p = s.G + ((int64_t)n * R + r) * s.ldg + f;
+    sum *= s.scale;
+    if (accumulate) sum += *(const f32x4*)p;
+    *(f32x4*)p = sum;
   }
-  if (!in) return;
-  float* p = s.G + ((int64_t)n * R + r) * s.ldg + f;
-  sum *= s.scale;
-  if (accumulate) sum += *(const f32x4*)p;
-  *(f32x4*)p = sum;
 }
 
 // Both weight gradients of few rows in one launch: a workgroup takes 128 features of one adapter, 16 ranks, and all rows that the adapter has, 32 in each of
@@ -1038,8 +1048,10 @@ hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOu
   // Chunks shared out among a workgroup's waves while that gives no more than 2048 workgroups, and where an adapter has more than eight in the mean
   const int64_t wide = (int64_t)((a.C + 1023) / 1024 + (b.C + 1023) / 1024) * R * g.adapters;
   const int shares = wide <= 512 && slots(g, chunk) > 8 * (int64_t)g.adapters ? 4 : 1, width = 1024 / shares, ablocks = (a.C + width - 1) / width, bblocks = (b.C + width - 1) / width;
+  // Workgroups for several ranks each where there are many: of a thousand adapters most may have no rows
+  const int64_t ranks = ablocks + bblocks > 0 && g.adapters > 0 ? 8192 / ((int64_t)(ablocks + bblocks) * g.adapters) : 1;
   if (ablocks + bblocks > 0 && g.adapters > 0)
-    SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_sum, dim3((unsigned)(ablocks + bblocks), (unsigned)R, (unsigned)g.adapters), dim3(256), s, g, R, chunk,
+    SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_sum, dim3((unsigned)(ablocks + bblocks), (unsigned)(ranks < 1 ? 1 : ranks < R ? ranks : R), (unsigned)g.adapters), dim3(256), s, g, R, chunk,
                 (OuterSum{x.part, a.G, a.ldg, a.m_scale, a.C}), (OuterSum{z.part, b.G, b.ldg, b.m_scale, b.C}), ablocks, shares, accumulate);
   return hipGetLastError();
 }

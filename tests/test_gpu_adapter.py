@@ -355,6 +355,22 @@ def test_wgrad_empty(sste):
     assert dA.shape == (2, 8, 0) and dB.shape == (2, 8, 0)
 
 
+@pytest.mark.parametrize("T", [64, 2300])
+def test_wgrad_leaves_adapters_without_rows(sste, T):
+    """accumulate: what an adapter without rows has stays as it is, bit for bit (negative zeros, NaN)."""
+    rng = np.random.default_rng(8)
+    X, dZ, S = normal(rng, (T, 64), 1).to(torch.bfloat16), normal(rng, (T, 72), 1).to(torch.bfloat16), normal(rng, (T, 16), 1)
+    dA, dB = normal(rng, (40, 16, 64), 1), normal(rng, (40, 16, 72), 1)
+    dA[3], dB[3], dA[39] = -0.0, float("nan"), -0.0
+    kept = dA.clone(), dB.clone()
+    sste.adapter_wgrad(dZ, X, S, S, *segments([0, 9, 30, 30, T - 2], [5, -1, 3, 7]), 40, dA=dA, dB=dB, accumulate=True)
+    for got, want in zip((dA, dB), kept):
+        same = (got.view(torch.int32) == want.view(torch.int32)).flatten(1)
+        assert not same[5].all() and not same[7].all()
+        same[[5, 7]] = True
+        assert same.all()
+
+
 def test_same_bits_every_time(sste):
     rng = np.random.default_rng(7)
     T = 9000
