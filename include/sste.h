@@ -598,10 +598,13 @@ int sste_flip_count(const void* meta_a, const void* meta_b, int64_t O, int64_t I
 /*
  * Per-kernel timing for benchmarks.  Between sste_timing_begin and sste_timing_end every launch of a
  * hot-path kernel is bracketed by its own pair of HIP events on the launch stream (events are host
- * objects; no device memory is allocated).  sste_timing_end waits for the recorded events, adds up
- * the elapsed milliseconds and the launch counts per kernel into arrays of SSTE_K_COUNT entries
- * (either may be NULL) and releases the events.  At most `max_launches` launches are recorded; later
- * ones run untimed.  Timing is process-wide; do not nest.
+ * objects; no device memory is allocated).  sste_timing_end_all waits for the recorded events, adds up
+ * the elapsed milliseconds and the launch counts per kernel into arrays of `entries` entries (either may
+ * be NULL; kernels beyond them are left out, entries beyond the kernels are 0) and releases the events.
+ * sste_timing_end does the same for the first SSTE_K_COUNT kernels.  That number stays as it is: the
+ * function has no other way of knowing the arrays of a program that an older header built.  Kernels that came later are
+ * numbered from it, up to SSTE_K_ALL - 1.  At most `max_launches` launches are recorded; later ones run untimed.  Timing
+ * is process-wide; do not nest.
  */
 typedef enum {
   SSTE_K_PROJECT_PACK = 0,   /* projection + scale + pack */
@@ -612,12 +615,14 @@ typedef enum {
   SSTE_K_DGRAD = 5,          /* input-gradient dense GEMM */
   SSTE_K_SGD_PROJECT_PACK = 6, /* dense-weight update fused with projection + pack */
   SSTE_K_CAST = 7,           /* per-tensor rescale + cast to an 8-bit format */
+  SSTE_K_COUNT = 8,          /* entries of sste_timing_end */
   SSTE_K_ADAPTER = 8,        /* low-rank adapters: both products of a call, or the weight gradients and their sum */
   SSTE_K_CHECKPOINT = 9,     /* activation checkpoints */
-  SSTE_K_COUNT = 10
+  SSTE_K_ALL = 10            /* entries of sste_timing_end_all that hold something */
 } sste_kernel_id;
 int sste_timing_begin(int max_launches);
 int sste_timing_end(double* total_ms, int* launches);
+int sste_timing_end_all(double* total_ms, int* launches, int entries);
 
 /* Message for the most recent non-OK status returned on the calling thread ("" if none). */
 const char* sste_last_error(void);

@@ -110,6 +110,8 @@ def library() -> ctypes.CDLL:
     lib.sste_timing_begin.restype = ci
     lib.sste_timing_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ci)]
     lib.sste_timing_end.restype = ci
+    lib.sste_timing_end_all.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ci), ci]
+    lib.sste_timing_end_all.restype = ci
     for name in ("sste_project_pack", "sste_sgd_project_pack", "sste_sgd_project_pack_batch_prepare", "sste_sgd_project_pack_batch", "sste_project_pack_batch_prepare", "sste_project_pack_batch", "sste_linear_fwd", "sste_linear_dgrad",
                  "sste_linear_wgrad", "sste_mvue_materialize", "sste_compute_beta", "sste_flip_count", "sste_cast_fp8"):
         getattr(lib, name).restype = ci
@@ -700,10 +702,10 @@ def timing_begin(max_launches: int = 4096) -> None:
 
 
 def timing_end():
-    """sste_timing_end: {kernel name: (total milliseconds, launches)} since timing_begin."""
+    """sste_timing_end_all: {kernel name: (total milliseconds, launches)} since timing_begin."""
     ms = (ctypes.c_double * len(KERNEL_NAMES))()
     n = (ctypes.c_int * len(KERNEL_NAMES))()
-    _check(library().sste_timing_end(ms, n))
+    _check(library().sste_timing_end_all(ms, n, len(KERNEL_NAMES)))
     return {name: (float(ms[i]), int(n[i])) for i, name in enumerate(KERNEL_NAMES)}
 
 

@@ -74,7 +74,7 @@ using namespace sste;
 
 extern "C" {
 
-int sste_version(void) { return 200; }
+int sste_version(void) { return 201; }
 
 int sste_timing_begin(int max_launches) {
   clear_error();
@@ -96,12 +96,15 @@ int sste_timing_begin(int max_launches) {
   return SSTE_OK;
 }
 
-int sste_timing_end(double* total_ms, int* launches) {
+int sste_timing_end(double* total_ms, int* launches) { return sste_timing_end_all(total_ms, launches, SSTE_K_COUNT); }
+
+int sste_timing_end_all(double* total_ms, int* launches, int entries) {
   clear_error();
+  if (entries < 0) return fail(SSTE_ERR_VALUE, "timing_end: negative number of entries");
   std::lock_guard<std::mutex> lk(g_timing_mu);
   if (!g_timing_on) return fail(SSTE_ERR_VALUE, "timing_end: timing is not on");
   g_timing_on = false;
-  for (int k = 0; k < SSTE_K_COUNT; k++) {
+  for (int k = 0; k < entries; k++) {
     if (total_ms) total_ms[k] = 0.0;
     if (launches) launches[k] = 0;
   }
@@ -112,7 +115,7 @@ int sste_timing_end(double* total_ms, int* launches) {
     if (e == hipSuccess) e = hipEventElapsedTime(&ms, g_slots[i].start, g_slots[i].stop);
     if (e != hipSuccess) { status = fail(SSTE_ERR_HIP, "timing_end: %s", hipGetErrorString(e)); break; }
     int k = g_slot_kind[i];
-    if (k >= 0 && k < SSTE_K_COUNT) {
+    if (k >= 0 && k < entries) {
       if (total_ms) total_ms[k] += (double)ms;
       if (launches) launches[k] += 1;
     }
