@@ -458,6 +458,17 @@ def cast_fp8(X: torch.Tensor, scale: float, out_dtype: int = F8E4M3, Q: Optional
     return (Q if store else None), amax_out
 
 
+# What a matrix of a format is kept in: the format's own type, or raw bits.  Other floating-point types of the same width are no such matrix.
+_RAW16, _RAW8 = (torch.int16, torch.uint16), (torch.uint8, torch.int8)
+_STORAGE = {BF16: (torch.bfloat16, *_RAW16), F8E4M3: (torch.float8_e4m3fn, *_RAW8), F8E5M2: (torch.float8_e5m2, *_RAW8), F8BLOCK: (torch.float8_e4m3fn, *_RAW8)}
+
+
+def _holds(t: torch.Tensor, dtype: int, name: str) -> None:
+    """Refuses a tensor of another type than the format's: its bits would be read as if they were.  (An unknown format is left to the library.)"""
+    if dtype in _STORAGE and t.dtype not in _STORAGE[dtype]:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in _STORAGE[dtype])}, not {t.dtype}")
+
+
 def _stack(t: torch.Tensor, itemsize: int, name: str) -> Tuple[int, int, int, int]:
     """(adapters, rank, width, leading dimension in elements) of a stack of matrices, one below the other."""
     if t.dim() != 3:
@@ -482,6 +493,8 @@ def _segments(row_start: torch.Tensor, seg_adapter: torch.Tensor) -> int:
 def _adapter_arguments(X, x_name, row_start, seg_adapter, A, B, scale, dtype):
     """What adapter_fwd and adapter_dgrad check alike: (T, width, ldx, segments, adapters, rank, I, lda, O, ldb)."""
     T, width, ldx = _matrix(X, _esize(dtype), x_name)
+    for t, kind, name in ((X, dtype, x_name), (A, BF16, "A"), (B, BF16, "B")):
+        _holds(t, kind, name)
     segments = _segments(row_start, seg_adapter)
     n, R, I, lda = _stack(A, 2, "A")
     n2, R2, O, ldb = _stack(B, 2, "B")
@@ -541,8 +554,8 @@ def adapter_fwd(X: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Ten
                 scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, dtype: int = BF16, x_scale: float = 1.0,
                 Z: Optional[torch.Tensor] = None, S: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """sste_adapter_fwd: S = scale_n x_scale X A_n^T (float32) and Z = base + S B_n (bf16), n the adapter of each row.  A is (adapters, rank, I)
-    and B (adapters, rank, O), bf16; rows row_start[s] .. row_start[s + 1] - 1 use adapter seg_adapter[s], or none (-1).  Z may be base.
-    Returns (Z, S)."""
+    and B (adapters, rank, O), bf16; rows row_start[s] .. row_start[s + 1] - 1 use adapter seg_adapter[s], or none (-1).  Z may be base.  X, A and B
+    are tensors of their format's own type, or of integers that hold its bits.  Returns (Z, S)."""
     T, I, ldx, segments, n, R, Ia, lda, O, ldb = _adapter_arguments(X, "X", row_start, seg_adapter, A, B, scale, dtype)
     if Ia != I:
         raise ValueError("A must be as wide as X")
@@ -587,6 +600,8 @@ def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.
     X holds the codes and x_blocks the scales of a checkpoint (checkpoint_pack).  Returns (dA (adapters, rank, I), dB (adapters, rank, O))."""
     T, O, lddz = _matrix(dZ, _esize(dtype), "dZ")
     T2, I, ldx = _matrix(X, _esize(x_dtype), "X")
+    _holds(dZ, dtype, "dZ")
+    _holds(X, x_dtype, "X")
     if T2 != T:
         raise ValueError("dZ and X must have the same number of rows (tokens)")
     segments = _segments(row_start, seg_adapter)
@@ -620,6 +635,7 @@ def checkpoint_pack(X: torch.Tensor, codes: Optional[torch.Tensor] = None, scale
     """sste_checkpoint_pack: X (bf16) as e4m3 codes with a power of two for every 32 features of a row.  Returns (codes (R, C) uint8,
     scales (R, ceil(C / 32)) uint8)."""
     R, C, ldx = _matrix(X, 2, "X")
+    _holds(X, BF16, "X")
     codes, ldc = _result(codes, R, C, torch.uint8, X, "codes")
     scales, lds = _result(scales, R, (C + 31) // 32, torch.uint8, X, "scales")
     with _together(X, codes, scales):
@@ -632,6 +648,7 @@ def checkpoint_backward(codes: torch.Tensor, scales: torch.Tensor, dA: Optional[
     """sste_checkpoint_backward: of the checkpointed H, A = act(H) (if restore) and dH = dA * act'(H) (if dA is given), both bf16.  With ACT_NONE, A is
     the checkpointed tensor itself.  dH may be dA.  Returns (A or None, dH or None)."""
     R, C, ldc = _matrix(codes, 1, "codes")
+    _holds(codes, F8BLOCK, "codes")
     lds = _given(scales, R, (C + 31) // 32, torch.uint8, "scales")
     lda = lddh = 0
     if restore:

@@ -135,6 +135,18 @@ Matrix matrix(Args& a, const at::Tensor* t, int itemsize) {
   m.p = t->numel() > 0 ? t->data_ptr() : nullptr;
   return m;
 }
+// a tensor of the format's own type, or its raw bits (_holds of binding.py)
+void holds(Args& a, const at::Tensor* t, int dtype) {
+  if (!a.ok || !t) return;
+  const at::ScalarType type = t->scalar_type();
+  const bool raw8 = type == at::kByte || type == at::kChar;
+  switch (dtype) {
+    case SSTE_BF16: a.ok = type == at::kBFloat16 || type == at::kShort || type == at::kUInt16; break;
+    case SSTE_F8E4M3:
+    case SSTE_F8BLOCK: a.ok = type == at::kFloat8_e4m3fn || raw8; break;
+    case SSTE_F8E5M2: a.ok = type == at::kFloat8_e5m2 || raw8; break;
+  }
+}
 // matrices one below the other: (adapters, rank, width)
 struct Stack {
   void* p = nullptr;
@@ -408,6 +420,9 @@ PyObject* adapter(Fn f, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnam
   const Matrix x = matrix(a, X, item(dt));
   const int64_t n_seg = segments(a, rs, sa);
   const Stack ma = stack(a, A, 2), mb = stack(a, B, 2);
+  holds(a, X, dt);
+  holds(a, A, SSTE_BF16);
+  holds(a, B, SSTE_BF16);
   if (!a.ok || ma.n != mb.n || ma.rank != mb.rank || (f == ADAPTER_FWD ? ma : mb).width != x.cols) return decline(f, args, nargs, kwnames);
   if (scale && (scale->dim() != 1 || scale->size(0) != ma.n || scale->scalar_type() != at::kFloat || !scale->is_cuda() || !scale->is_contiguous())) return decline(f, args, nargs, kwnames);
   const int64_t C = (f == ADAPTER_FWD ? mb : ma).width;
@@ -467,6 +482,8 @@ PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
   const int acc = !o[14] || o[14] == Py_False ? 0 : 1;
   if (o[14] && o[14] != Py_True && o[14] != Py_False) a.ok = false;
   const Matrix y = matrix(a, dZ, item(dt)), x = matrix(a, X, item(xdt));
+  holds(a, dZ, dt);
+  holds(a, X, xdt);
   const int64_t n_seg = segments(a, rs, sa);
   if (!a.ok || S->dim() != 2 || y.rows != x.rows || n < 0 || (acc && !(dA && dB))) return decline(ADAPTER_WGRAD, args, nargs, kwnames);
   const int64_t R = S->size(1);
@@ -510,6 +527,7 @@ PyObject* checkpoint_pack(PyObject*, PyObject* const* args, Py_ssize_t nargs, Py
   if (!g_bound || !collect(n_pack8, args, nargs, kwnames, o)) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
   const at::Tensor *X = a.needed(o[0]), *codes = a.tensor(o[1]), *scales = a.tensor(o[2]);
   const Matrix x = matrix(a, X, 2);
+  holds(a, X, SSTE_BF16);
   if (!a.ok) return decline(CHECKPOINT_PACK, args, nargs, kwnames);
   const int64_t blocks = (x.cols + 31) / 32;
   at::Tensor made_c, made_s;
@@ -539,6 +557,7 @@ PyObject* checkpoint_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs
   const bool restore = !o[6] || o[6] == Py_True;
   if ((o[6] && o[6] != Py_True && o[6] != Py_False) || (!restore && A) || (!dA && dH)) a.ok = false;
   const Matrix c = matrix(a, codes, 1), b = exactly(a, scales, c.rows, (c.cols + 31) / 32, at::kByte), d = exactly(a, dA, c.rows, c.cols, at::kBFloat16);
+  holds(a, codes, SSTE_F8BLOCK);
   if (!a.ok) return decline(CHECKPOINT_BACKWARD, args, nargs, kwnames);
   at::Tensor made_a, made_h;
   if (restore && !A) made_a = make(*codes, c.rows, c.cols, at::kBFloat16), A = &made_a;
