@@ -512,8 +512,8 @@ int sste_cast_fp8(const void* X, int64_t R, int64_t C, int64_t ldx, int out_dtyp
  *   sste_adapter_wgrad   dA_n (+)= x_scale * sum dS^T X         dB_n (+)= dz_scale * sum S^T dZ  sums over the rows of adapter n
  *
  * S and dS (T x R, float32) are outputs of the first two calls that the third takes; both contain scale_n, which is why dA and dB need it
- * no more.  Products are accumulated in float32; S enters S B_n as the sum of two bf16, to within 2^-17 of
- * itself (dS likewise), and the sums over rows as the sum of three, with all its bits.
+ * no more.  Products are accumulated in float32.  S and dS enter the products with B and A, and the sums over
+ * rows, as sums of three bf16, with all their bits.
  *
  *   row_start    in  device, int32, segments + 1 entries that do not decrease: segment s holds the rows row_start[s] .. row_start[s+1] - 1
  *                    (a request, a sequence, a single token; empty ones are allowed)

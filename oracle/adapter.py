@@ -10,16 +10,15 @@ Rows come in segments: segment s holds the rows row_start[s] .. row_start[s + 1]
     weight gradients  dA_n = sum dS^T X         dB_n = sum S^T dZ       over the rows of adapter n
 
 `apply` is the forward pass; with dZ for X and A and B exchanged it is the input gradient.  Every result comes with a bound on what float32
-accumulation and the operands' split into two bf16 may cost (`_bound` results): a dot product of n terms accumulated in float32, whatever the
-order and even if the adder truncates, is off by at most n 2^-23 sum |a b|; a float32 number as the sum of two bf16 by 2^-17 of itself, of three by 2^-24.
+accumulation and the operands' split into three bf16 may cost (`_bound` results): a dot product of n terms accumulated in float32, whatever the
+order and even if the adder truncates, is off by at most n 2^-23 sum |a b|; a float32 number as the sum of three bf16 by 2^-24 of itself.
 """
 import numpy as np
 
 ACCUMULATE = 2.0 ** -23          # of one addition
-# x in [2^e, 2^(e+1)): bf16 has 8 significant bits there, steps of 2^(e-7), so hi is off by at most 2^(e-8).  What is left is below that in
-# magnitude, in steps of at most 2^(e-9-7), so lo is off by at most 2^(e-17): 2^-17 of x, reached just below the end of a binade of what is left.
-SPLIT = 2.0 ** -17
-SPLIT3 = 2.0 ** -24              # a third part takes what is left: 24 bits and more
+# x in [2^e, 2^(e+1)): bf16 has 8 significant bits there, so what the first part leaves has 16 below 2^(e-8) or so, what the second leaves 8 below 2^(e-16): nothing
+# is left of them by the third, but for numbers so small that bf16 ends above their last bits.
+SPLIT3 = 2.0 ** -24
 
 
 def rows_of(row_start, seg_adapter, adapters, T):
@@ -44,7 +43,7 @@ def apply(X, ids, down, up, scale, base):
         S[at] = s * (X[at] @ down[n].T)
         eS[at] = abs(s) * ((X.shape[1] + 16) * ACCUMULATE) * (np.abs(X[at]) @ np.abs(down[n]).T)      # 16: the waves' sums, scale and its product
         out[at] += S[at] @ up[n]
-        eO[at] = (eS[at] + (SPLIT + (2 * R + 2) * ACCUMULATE) * np.abs(S[at])) @ np.abs(up[n])
+        eO[at] = (eS[at] + (SPLIT3 + (3 * R + 2) * ACCUMULATE) * np.abs(S[at])) @ np.abs(up[n])
         if base is not None:
             eO[at] += ACCUMULATE * np.abs(base[at])
     return out, S, eS, eO

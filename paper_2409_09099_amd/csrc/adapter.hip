@@ -117,18 +117,18 @@ __device__ __forceinline__ bf16x8 frag(uint4 v) {
   __builtin_memcpy(&r, &v, 16);
   return r;
 }
-// A float as the sum of bf16.  One alone would be off by up to 2^-8, a rounding of a 32-bit sum that nothing asks for; the matrix instructions that the
-// others take are hidden under the memory traffic.  hi (the nearest) and lo (the nearest to what is left) are off by at most 2^-17, which the bf16 results
-// of `up` do not show; with a third part nothing is lost, for the weight gradients, whose float32 results would.
+// Two floats as sums of three bf16 each, which have all of their bits: S and dS are 32-bit sums, and neither the weight gradients nor the products with B and A
+// are to see them rounded (where base and S B cancel, a bf16 result shows even two parts' 2^-17).
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  hi = bf16_rne_pack(a, b);
+  a -= bf16lo_f32(hi), b -= bf16hi_f32(hi);
+  mid = bf16_rne_pack(a, b);
+  lo = bf16_rne_pack(a - bf16lo_f32(mid), b - bf16hi_f32(mid));
+}
 __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& mid, uint4& lo) {
   uint32_t h[4], m[4], l[4];
 #pragma unroll
-  for (int p = 0; p < 4; p++) {
-    h[p] = bf16_rne_pack(x[2 * p], x[2 * p + 1]);
-    const float a = x[2 * p] - bf16lo_f32(h[p]), b = x[2 * p + 1] - bf16hi_f32(h[p]);
-    m[p] = bf16_rne_pack(a, b);
-    l[p] = bf16_rne_pack(a - bf16lo_f32(m[p]), b - bf16hi_f32(m[p]));
-  }
+  for (int p = 0; p < 4; p++) split2(x[2 * p], x[2 * p + 1], h[p], m[p], l[p]);
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   mid = make_uint4(m[0], m[1], m[2], m[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
@@ -300,11 +300,11 @@ struct UpArgs {
   int64_t ldout;
 };
 
-// A tile's rows of D as the sum of two bf16, and the features of a wave.
+// A tile's rows of D as the sum of three bf16, and the features of a wave.
 template <int RP, int TT>
 struct Up {
   static constexpr int TR = TT * 16, LDP = RP + 8, SETS = RP <= 32 ? 1 : RP / 32;
-  uint16_t parts[2][TR][LDP];
+  uint16_t parts[3][TR][LDP];
 
   // What a wave loads of its features before it needs the tile's D: the first 32 ranks of the adapter, and its rows of base.
   struct Ahead {
@@ -331,13 +331,12 @@ struct Up {
       for (int i = 0; i < 4; i++) a.old[j][i] = buffer_load_b128(rb, at + (uint32_t)(j * 16 + 4 * q + i) * (uint32_t)o.ldbase * 2, 0);
   }
   __device__ __forceinline__ void put(int row, int c, f32x4 v) {
-    uint2 hi, lo;
-    hi.x = bf16_rne_pack(v[0], v[1]);
-    hi.y = bf16_rne_pack(v[2], v[3]);
-    lo.x = bf16_rne_pack(v[0] - bf16lo_f32(hi.x), v[1] - bf16hi_f32(hi.x));
-    lo.y = bf16_rne_pack(v[2] - bf16lo_f32(hi.y), v[3] - bf16hi_f32(hi.y));
+    uint2 hi, mid, lo;
+    split2(v[0], v[1], hi.x, mid.x, lo.x);
+    split2(v[2], v[3], hi.y, mid.y, lo.y);
     *(uint2*)&parts[0][row][c] = hi;
-    *(uint2*)&parts[1][row][c] = lo;
+    *(uint2*)&parts[1][row][c] = mid;
+    *(uint2*)&parts[2][row][c] = lo;
   }
   // Features f0 .. f0 + 127.  Lane (m, q) loads eight neighbouring features of ranks 8 q .. 8 q + 7 in eight pieces of 16 bytes and transposes them in
   // registers: the operands of eight matrix instructions, the j-th for features 8 m + j, so that the results of one row lie 8 in a lane and 128 in 16
@@ -358,17 +357,16 @@ struct Up {
         if (s == 0)
 #pragma unroll
           for (int j = 0; j < 8; j++) c[j] = (f32x4){0, 0, 0, 0};
-        if (RP == 16) {                                  // hi and lo of 16 ranks fill one instruction's 32 places
-          const uint4 d = *(const uint4*)&parts[q >> 1][k * 16 + m][(q & 1) * 8];
+        // Of 16 ranks, hi and mid fill one instruction's 32 places, lo half of another's
+        const int row = k * 16 + m, at_rank = RP == 16 ? (q & 1) * 8 : s * 32 + q * 8;
+        const uint4 hi = *(const uint4*)&parts[RP == 16 ? q >> 1 : 0][row][at_rank], mid = *(const uint4*)&parts[1][row][at_rank];
+        uint4 lo = *(const uint4*)&parts[2][row][at_rank];
+        if (RP == 16 && q >= 2) lo = make_uint4(0, 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < 8; j++) c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(d), frag(u[j]), c[j], 0, 0, 0);
-        } else {
-          const uint4 hi = *(const uint4*)&parts[0][k * 16 + m][s * 32 + q * 8], lo = *(const uint4*)&parts[1][k * 16 + m][s * 32 + q * 8];
-#pragma unroll
-          for (int j = 0; j < 8; j++) {
-            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(u[j]), c[j], 0, 0, 0);
-            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(u[j]), c[j], 0, 0, 0);
-          }
+        for (int j = 0; j < 8; j++) {
+          c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(hi), frag(u[j]), c[j], 0, 0, 0);
+          if (RP > 16) c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(mid), frag(u[j]), c[j], 0, 0, 0);
+          c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(lo), frag(u[j]), c[j], 0, 0, 0);
         }
         if (s + 1 < SETS) continue;
 #pragma unroll
