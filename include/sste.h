@@ -513,7 +513,7 @@ int sste_cast_fp8(const void* X, int64_t R, int64_t C, int64_t ldx, int out_dtyp
  *
  * S and dS (T x R, float32) are outputs of the first two calls that the third takes; both contain scale_n, which is why dA and dB need it
  * no more.  Products are accumulated in float32.  S and dS enter the products with B and A, and the sums over
- * rows, as sums of three bf16, with all their bits.
+ * rows, as sums of three bf16, with all their bits (from 2^-110 up).
  *
  *   row_start    in  device, int32, segments + 1 entries that do not decrease: segment s holds the rows row_start[s] .. row_start[s+1] - 1
  *                    (a request, a sequence, a single token; empty ones are allowed)

@@ -16,8 +16,8 @@ order and even if the adder truncates, is off by at most n 2^-23 sum |a b|; a fl
 import numpy as np
 
 ACCUMULATE = 2.0 ** -23          # of one addition
-# x in [2^e, 2^(e+1)): bf16 has 8 significant bits there, so what the first part leaves has 16 below 2^(e-8) or so, what the second leaves 8 below 2^(e-16): nothing
-# is left of them by the third, but for numbers so small that bf16 ends above their last bits.
+# The first part takes the upper 8 of 24 bits, the second the next 8, the third the rest: nothing is lost from 2^-110 up, where bf16's smallest number is the
+# last bit's.  2^-24 leaves room for any way of splitting in three.
 SPLIT3 = 2.0 ** -24
 
 

@@ -118,12 +118,17 @@ __device__ __forceinline__ bf16x8 frag(uint4 v) {
   return r;
 }
 // Two floats as sums of three bf16 each, which have all of their bits: S and dS are 32-bit sums, and neither the weight gradients nor the products with B and A
-// are to see them rounded (where base and S B cancel, a bf16 result shows even two parts' 2^-17).
+// are to see them rounded (where base and S B cancel, a bf16 result shows even two parts' 2^-17).  Each part is cut off, not rounded: 8 of 24 bits, 8 of the
+// 16 that are left, and the last 8; rounded up, the first would be infinite from 2^128 (1 - 2^-9) on.
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  hi = bf16_rne_pack(a, b);
-  a -= bf16lo_f32(hi), b -= bf16hi_f32(hi);
-  mid = bf16_rne_pack(a, b);
-  lo = bf16_rne_pack(a - bf16lo_f32(mid), b - bf16hi_f32(mid));
+  const auto cut = [&] {
+    const uint32_t r = __builtin_amdgcn_perm(f2u(b), f2u(a), 0x07060302u);
+    a -= bf16lo_f32(r), b -= bf16hi_f32(r);
+    return r;
+  };
+  hi = cut();
+  mid = cut();
+  lo = cut();
 }
 __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& mid, uint4& lo) {
   uint32_t h[4], m[4], l[4];

@@ -66,3 +66,43 @@ def test_every_bit_of_the_low_rank_product_counts(sste, T, K, C, R, count, fwd, 
     want[:, full], want[:, upper] = v, low - v
     assert np.array_equal(S.cpu().numpy(), want)
     assert np.array_equal(out.float().cpu().numpy(), np.repeat(low[:, None], C, 1))
+
+
+def test_products_with_the_largest_floats(sste):
+    """S is the largest float32 in one row: it enters the second product as it is, not as the infinity that bf16 rounds it to."""
+    T, K, C, R = 20, 64, 136, 16
+    X, A, B = torch.zeros((T, K), device="cuda"), torch.zeros((1, R, K), device="cuda"), torch.zeros((1, R, C), device="cuda")
+    X[3, :8] = 7 * 2.0 ** 52                                              # eight digits of three bits: 2^24 - 1, times 2^104
+    A[0, 5, :8] = 2.0 ** 52 * 8.0 ** torch.arange(8, device="cuda")
+    B[0, 5] = 2.0 ** -104
+    X, A, B = (t.to(torch.bfloat16) for t in (X, A, B))
+    rows = torch.tensor([0, T], dtype=torch.int32, device="cuda"), torch.tensor([0], dtype=torch.int32, device="cuda")
+    Z, S = sste.adapter_fwd(X, *rows, A, B)
+    assert S[3, 5] == torch.finfo(torch.float32).max and S.count_nonzero() == 1
+    assert (Z[3] == 2.0 ** 24).all() and not Z[:3].any() and not Z[4:].any()
+    dX, dS = sste.adapter_dgrad(X, *rows, B, A)
+    assert torch.equal(dX, Z) and torch.equal(dS, S)
+
+
+@pytest.mark.parametrize("T", [400, 2400])                               # in one launch and in two
+def test_gradients_of_every_exponent(sste, T):
+    """S = (1 + 2^-23) 2^e: both its bits arrive, up to the largest floats and down to 2^-110 (its last bit is then the smallest bf16)."""
+    R, I, O = 8, 64, 72
+    exponents = np.arange(-110, 128)
+    N = len(exponents)
+    value, other = (torch.from_numpy(np.ldexp(m, n)).cuda() for m, n in ((1 + 2.0 ** -23, exponents), (1.0, -exponents.clip(-100, 100))))      # exactly: on the host
+    S = torch.zeros((T, R), device="cuda")
+    S[:N, 3] = value.float()
+    S[N - 1, 4] = torch.finfo(torch.float32).max
+    M = torch.zeros((T, O), device="cuda")
+    M[:N] = other.float()[:, None]
+    M = M.to(torch.bfloat16)
+    starts = torch.arange(N + 1, dtype=torch.int32, device="cuda")
+    ids = torch.arange(N, dtype=torch.int32, device="cuda")
+    dA, dB = sste.adapter_wgrad(M, M[:, :I].contiguous(), S, S, starts, ids, N)
+    want = torch.zeros((N, R), device="cuda", dtype=torch.float64)
+    want[:, 3] = value * other
+    want[N - 1, 4] = torch.finfo(torch.float32).max * other[N - 1]
+    for G in (dA, dB):
+        wrong = (G.double() != want[:, :, None]).any(2).any(1)
+        assert not wrong.any(), exponents[wrong.cpu().numpy()]
