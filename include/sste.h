@@ -553,10 +553,12 @@ size_t sste_adapter_workspace_bytes(int64_t T, int64_t segments, int64_t R, int6
  * The adapters' weight gradients.  X may also be a checkpoint (x_dtype SSTE_F8BLOCK: codes in X, scales in x_blocks with leading dimension ldxb,
  * x_scale 1); otherwise x_blocks is ignored.  dA (adapters * R x I, ldda) and dB (adapters * R x O, lddb) are float32, leading dimensions multiples
  * of 4; an adapter without rows gets zeros, or keeps what it has with accumulate = 1.  S and dS of rows without an adapter are not read.
- * Each adapter's rows are summed in a fixed order, in chunks that depend on the sizes and the bounds: the same call gives the same bits.
- * workspace: sste_adapter_wgrad_workspace_bytes(T, segments, R, I, O) bytes of device scratch, 16-byte aligned (0 on bad arguments, and where few rows
- * need none): R x (I + O) floats for each chunk, and every segment is one at least, so a batch for training has its rows sorted by adapter, or in long
- * segments.
+ * Each adapter's rows are summed in a fixed order, in parts that depend on the sizes and the bounds: the same call gives the same bits.
+ * workspace: sste_adapter_wgrad_workspace_bytes_ex(T, segments, adapters, R, I, O) bytes of device scratch, 16-byte aligned (0 on bad arguments, and where
+ * few rows need none).  Rows are summed in chunks of a segment's rows, R x (I + O) floats for each, or, where short segments would make that more than one for
+ * each adapter and 2048 rows of the batch, in such blocks of rows: R x (I + O) floats for each adapter of a block (none of a single block), and an integer
+ * for each row and each of these sums.
+ * sste_adapter_wgrad_workspace_bytes does not know the adapters and is enough for any number of them.
  */
 int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
                        const void* X, int64_t I, int64_t ldx, int x_dtype, float x_scale, const void* x_blocks, int64_t ldxb,
@@ -565,6 +567,7 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
                        float* dA, int64_t ldda, float* dB, int64_t lddb, int accumulate,
                        void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t sste_adapter_wgrad_workspace_bytes(int64_t T, int64_t segments, int64_t R, int64_t I, int64_t O);
+size_t sste_adapter_wgrad_workspace_bytes_ex(int64_t T, int64_t segments, int64_t adapters, int64_t R, int64_t I, int64_t O);
 
 /*
  * Activation checkpoints in 8 bits: what the forward pass leaves for the backward pass (a layer's input, the pre-activations of the feed-forward

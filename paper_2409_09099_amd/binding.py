@@ -102,6 +102,8 @@ def library() -> ctypes.CDLL:
     lib.sste_adapter_wgrad.restype = ci
     lib.sste_adapter_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
     lib.sste_adapter_wgrad_workspace_bytes.restype = sz
+    lib.sste_adapter_wgrad_workspace_bytes_ex.argtypes = [i64, i64, i64, i64, i64, i64]
+    lib.sste_adapter_wgrad_workspace_bytes_ex.restype = sz
     lib.sste_checkpoint_pack.argtypes = [vp, i64, i64, i64, vp, i64, vp, i64, vp]
     lib.sste_checkpoint_pack.restype = ci
     lib.sste_checkpoint_backward.argtypes = [vp, vp, i64, i64, i64, i64, ci, vp, i64, vp, i64, vp, i64, vp]
@@ -588,8 +590,11 @@ def adapter_dgrad(dZ: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.
     return dX, dS
 
 
-def adapter_wgrad_workspace_bytes(T: int, segments: int, R: int, I: int, O: int) -> int:
-    return int(library().sste_adapter_wgrad_workspace_bytes(T, segments, R, I, O))
+def adapter_wgrad_workspace_bytes(T: int, segments: int, R: int, I: int, O: int, adapters: Optional[int] = None) -> int:
+    """sste_adapter_wgrad_workspace_bytes_ex; without the number of adapters, enough for any."""
+    if adapters is None:
+        return int(library().sste_adapter_wgrad_workspace_bytes(T, segments, R, I, O))
+    return int(library().sste_adapter_wgrad_workspace_bytes_ex(T, segments, adapters, R, I, O))
 
 
 def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.Tensor, row_start: torch.Tensor, seg_adapter: torch.Tensor,
@@ -623,7 +628,7 @@ def adapter_wgrad(dZ: torch.Tensor, X: torch.Tensor, S: torch.Tensor, dS: torch.
     if (na, Ra, Ia, nb, Rb, Ob) != (adapters, R, I, adapters, R, O) or dA.dtype != torch.float32 or dB.dtype != torch.float32:
         raise ValueError("dA and dB must be float32 tensors (adapters, rank, I) and (adapters, rank, O)")
     if workspace is None:
-        workspace = torch.empty(adapter_wgrad_workspace_bytes(T, segments, R, I, O), dtype=torch.uint8, device=X.device)
+        workspace = torch.empty(adapter_wgrad_workspace_bytes(T, segments, R, I, O, adapters), dtype=torch.uint8, device=X.device)
     with _together(dZ, X, S, dS, row_start, seg_adapter, x_blocks if x_dtype == F8BLOCK else None, dA, dB, workspace):
         _check(library().sste_adapter_wgrad(_ptr(dZ), T, O, lddz, dtype, dy_scale, _ptr(X), I, ldx, x_dtype, x_scale, _ptr(x_blocks), ldxb, _ptr(S), lds,
                                             _ptr(dS), ldds, _ptr(row_start), segments, _ptr(seg_adapter), adapters, R, _ptr(dA), ldda, _ptr(dB), lddb,
@@ -732,7 +737,7 @@ _PYTHON = {f.__name__: f for f in (project_pack, sgd_project_pack, linear_fwd, l
 _NATIVE_ENTRY_POINTS = ("sste_project_pack_gamma", "sste_sgd_project_pack", "sste_linear_fwd_ex", "sste_linear_fwd_act", "sste_linear_dgrad_act",
                         "sste_linear_wgrad_at", "sste_wgrad_workspace_bytes", "sste_cast_fp8", "sste_project_pack_batch",
                         "sste_sgd_project_pack_batch", "sste_adapter_fwd", "sste_adapter_dgrad", "sste_adapter_wgrad",
-                        "sste_adapter_workspace_bytes", "sste_adapter_wgrad_workspace_bytes", "sste_checkpoint_pack", "sste_checkpoint_backward", "sste_last_error")
+                        "sste_adapter_workspace_bytes", "sste_adapter_wgrad_workspace_bytes_ex", "sste_checkpoint_pack", "sste_checkpoint_backward", "sste_last_error")
 
 
 def _native_doc(f) -> str:

@@ -776,14 +776,13 @@ k_adapter_outer_sum(AdapterSegments g, int R, int chunk, OuterSum a, OuterSum b,
 // last the list repeats it, with zeros of L.  The waves' sums meet in LDS, in the order of the rows.
 // Bound by the launch and the waits in a row: the bounds, the rows of L and M, the stores (4 rows of 80 + 80, rank 16: 3.8 us; 256 rows of 1280 + 5120, rank
 // 128, of one adapter 7.1, of seven 20).
-constexpr int kFewRows = 2048, kFewSegments = 256;
 struct RowList {
   int start[kFewSegments + 1], adapter[kFewSegments], counts[kFewRows / 64];
   int rows[kFewRows + 8];
 
   // Lists the rows of adapter n and returns their number.
   __device__ __forceinline__ int find(const AdapterSegments& g, int n) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x;
     bool some = false;
     if (tid < g.segments) {
       const int v = g.adapter[tid];
@@ -804,8 +803,25 @@ struct RowList {
           if (lo + step <= g.segments && start[lo + step - 1] <= row) lo += step;
         mine[j] = __ballot(row < g.T && lo > 0 && row < start[lo] && adapter[max(lo - 1, 0)] == n);
       }
-      if (lane == 0) counts[j * 8 + wave] = __popcll(mine[j]);
     }
+    return list(mine, 0);
+  }
+  // The same for the kFewRows rows from row0 on, with a table of every row's adapter
+  __device__ __forceinline__ int find(const int* ids, int row0, int T, int n) {
+    uint64_t mine[kFewRows / 512];
+#pragma unroll
+    for (int j = 0; j < kFewRows / 512; j++) {
+      const int row = row0 + j * 512 + (int)threadIdx.x;
+      mine[j] = __ballot(row < T && ids[min(row, T - 1)] == n);
+    }
+    return list(mine, row0);
+  }
+  // `mine`: of 512 rows each, those of the wave's 64 that are listed
+  __device__ __forceinline__ int list(const uint64_t (&mine)[kFewRows / 512], int row0) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < kFewRows / 512; j++) counts[j * 8 + wave] = __popcll(mine[j]);
     __syncthreads();
     int total = 0, at[kFewRows / 512];
 #pragma unroll
@@ -817,9 +833,9 @@ struct RowList {
     for (int j = 0; j < kFewRows / 512; j++)
       if (mine[j] >> lane & 1) {
         const int to = at[j] + __popcll(mine[j] & ((1ull << lane) - 1));
-        rows[to] = j * 512 + tid;
+        rows[to] = row0 + j * 512 + tid;
         if (to == total - 1)
-          for (int i = 1; i < 8; i++) rows[to + i] = j * 512 + tid;
+          for (int i = 1; i < 8; i++) rows[to + i] = row0 + j * 512 + tid;
       }
     __syncthreads();
     return uniform(total);
@@ -885,6 +901,56 @@ k_adapter_outer_few(AdapterSegments g, OuterArgs x, OuterArgs z, OuterSum gx, Ou
   if (count == 0 && accumulate) return;
   if (a.type == M_BF16) few.run<false>(count, a, s, n, fb, rank0, R, accumulate);
   else few.run<true>(count, a, s, n, fb, rank0, R, accumulate);
+}
+
+// Many segments, for each of which chunks would take a sum: a table of every row's adapter first, then kFewRows rows at a time as above, and, of several such
+// blocks, their sums in order.  Bound by the waits in a row of three launches and by the sums; M is read once for 16 ranks.  16384 rows of 4096 + 4096, rank 16,
+// four adapters: 68 us in 1024 segments (4.0 TB/s; chunks 442), 74 in 16384 (chunks 6645), but 67 in eight, which chunks do in 60; 256 rows of 1280 + 5120,
+// rank 128, one adapter in 256 segments: 11 us (chunks 491).
+__global__ void __launch_bounds__(256)
+k_adapter_row_ids(AdapterSegments g, int* __restrict__ ids) {
+  const int row = (int)blockIdx.x * 256 + (int)threadIdx.x;
+  if (row >= g.T) return;
+  int lo = 0;                                            // as RowList::find
+  for (int step = 1 << (31 - __builtin_clz(g.segments)); step > 0; step >>= 1)
+    if (lo + step <= g.segments && g.row_start[lo + step - 1] <= row) lo += step;
+  ids[row] = lo > 0 && row < g.row_start[lo] ? g.adapter[lo - 1] : -1;
+}
+// gx, gz: the gradients themselves of one block of rows, otherwise the blocks' sums, adapter n of block b at number b * adapters + n
+__global__ void __launch_bounds__(512, 4)
+k_adapter_outer_rows(AdapterSegments g, OuterArgs x, OuterArgs z, OuterSum gx, OuterSum gz, int R, int accumulate, const int* __restrict__ ids, int* __restrict__ counts) {
+  __shared__ __align__(16) OuterFew few;
+  const int fblocks = x.fblocks + z.fblocks, block = (int)blockIdx.x / fblocks, n = blockIdx.z, to = block * (int)gridDim.z + n;
+  int fb = (int)blockIdx.x - block * fblocks;
+  const bool second = fb >= x.fblocks;
+  const OuterArgs a = second ? z : x;
+  const OuterSum s = second ? gz : gx;
+  const int count = uniform(few.list.find(ids, block * kFewRows, g.T, n));
+  if (counts && fb == 0 && blockIdx.y == 0 && threadIdx.x == 0) counts[to] = count;
+  if (second) fb -= x.fblocks;
+  if (count == 0 && (counts || accumulate)) return;      // a block's sum that there is not is not read
+  if (a.type == M_BF16) few.run<false>(count, a, s, to, fb, blockIdx.y * 16, R, accumulate);
+  else few.run<true>(count, a, s, to, fb, blockIdx.y * 16, R, accumulate);
+}
+__global__ void __launch_bounds__(256)
+k_adapter_outer_rows_sum(int R, int blocks, OuterSum a, OuterSum b, int ablocks, const int* __restrict__ counts, int accumulate) {
+  const bool second = (int)blockIdx.x >= ablocks;
+  const OuterSum s = second ? b : a;
+  const int f = ((second ? (int)blockIdx.x - ablocks : (int)blockIdx.x) * 256 + (int)threadIdx.x) * 4, r = blockIdx.y, n = blockIdx.z, adapters = gridDim.z;
+  if (f >= s.C) return;
+  f32x4 sum = {0, 0, 0, 0};
+  bool rows_of_it = false;
+  for (int k = 0; k < blocks; k++) {
+    const int64_t from = (int64_t)k * adapters + n;
+    if (counts[from] == 0) continue;
+    rows_of_it = true;
+    sum += *(const f32x4*)(s.part + (from * R + r) * s.C + f);
+  }
+  float* p = s.G + ((int64_t)n * R + r) * s.ldg + f;
+  if (accumulate && !rows_of_it) return;
+  sum *= s.scale;
+  if (accumulate) sum += *(const f32x4*)p;
+  *(f32x4*)p = sum;
 }
 
 int mode(int dtype) { return dtype == SSTE_F8E4M3 ? M_E4M3 : dtype == SSTE_F8E5M2 ? M_E5M2 : dtype == SSTE_F8BLOCK ? M_BLOCK : M_BF16; }
@@ -979,12 +1045,6 @@ void apply(const AdapterApply& a, hipStream_t s) {
   }
 }
 
-// One launch without chunks: its work grows with the adapters, for which the segments stand, and it reads M again for every 16 ranks.  Over 560 problems (64
-// to 2048 rows, 160 to 8192 features, ranks 16 to 128, 1 to 64 segments) the limit costs 0.8 % over the faster way in the mean, chunks everywhere 52 %.  64 rows
-// of 1280 + 5120, rank 64, nine segments: 5 us against 20; 2048 rows, one segment: 23 against 20.
-bool outer_few(int64_t T, int64_t segments, int R, int64_t I, int64_t O) {
-  return T <= kFewRows && segments <= kFewSegments && T * R * (I + O) * (segments > 8 ? segments : 8) <= 6000000000ll;
-}
 // Rows of a chunk of the weight gradients: about 384 workgroups of 256 features, one round of what fits the chip (16384 rows of 1024 + 4096, rank 16: 44.4 us;
 // 256 workgroups 50.2, 512 46.7; 7777 ragged rows of 1280 + 5120, rank 64: 47.0, 52.1 and 54.2).  A chunk's sum has R / rows times four of its rows' bytes,
 // written and read again: where 384 give fewer than 4 R rows (rank 64, 4096 rows of 1280 + 1280: 19.6 us, with half of them 23.2), 4 R unless that leaves
@@ -1020,22 +1080,39 @@ size_t adapter_apply_workspace_bytes(int64_t T, int segments, int R, int64_t K, 
 }
 
 size_t adapter_wgrad_workspace_bytes(int64_t T, int segments, int R, int64_t I, int64_t O) {
-  if (T == 0 || outer_few(T, segments, R, I, O)) return 0;
+  if (T == 0 || wgrad_few(T, segments, segments, R, I, O)) return 0;
   const AdapterSegments g = {nullptr, nullptr, segments, 0, (int)T};
   return (size_t)slots(g, outer_chunk(T, R, I, O)) * (size_t)R * (size_t)(I + O) * 4;
 }
 
 hipError_t launch_adapter_wgrad(const AdapterSegments& g, int R, const AdapterOuter& a, const AdapterOuter& b, int accumulate, void* ws, hipStream_t s) {
-  const bool few = outer_few(g.T, g.segments, R, a.C, b.C);
-  const int chunk = few ? 0 : outer_chunk(g.T, R, a.C, b.C), span = few ? 128 : 256;
+  const AdapterWgradWay way = wgrad_way(g.T, g.segments, g.adapters, R, a.C, b.C);
+  const int chunk = way == kWgradChunks ? outer_chunk(g.T, R, a.C, b.C) : 0, span = way == kWgradChunks ? 256 : 128;
   const auto args = [&](const AdapterOuter& o, float* part) {
     return OuterArgs{o.L, o.ldl, (const uint8_t*)o.M, o.ldm, mode(o.m_dtype), o.blocks, o.ldblocks, o.C, (o.C + span - 1) / span, part};
   };
-  if (few) {
+  if (way == kWgradFew) {
     const OuterArgs x = args(a, nullptr), z = args(b, nullptr);
     const OuterSum gx = {nullptr, a.G, a.ldg, a.m_scale, a.C}, gz = {nullptr, b.G, b.ldg, b.m_scale, b.C};
     const dim3 grid((unsigned)(x.fblocks + z.fblocks), (unsigned)((R + 15) / 16), (unsigned)g.adapters);
     if (grid.x > 0 && grid.z > 0) SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_few, grid, dim3(512), s, g, x, z, gx, gz, R, accumulate);
+    return hipGetLastError();
+  }
+  if (way == kWgradRows) {
+    const int blocks = (int)wgrad_row_blocks(g.T);
+    const int64_t sums = (int64_t)blocks * g.adapters;
+    int *ids = (int*)ws, *counts = blocks > 1 ? ids + g.T : nullptr;
+    float* part = (float*)ws + (g.T + sums + 3) / 4 * 4;      // of several blocks
+    const OuterArgs x = args(a, nullptr), z = args(b, nullptr);
+    const OuterSum gx = {part, a.G, a.ldg, a.m_scale, a.C}, gz = {part + sums * R * a.C, b.G, b.ldg, b.m_scale, b.C};
+    const auto block_sum = [&](const OuterSum& o) { return blocks > 1 ? OuterSum{nullptr, (float*)o.part, o.C, 1.0f, o.C} : o; };
+    if (g.adapters == 0) return hipSuccess;
+    SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_row_ids, dim3((unsigned)((g.T + 255) / 256)), dim3(256), s, g, ids);
+    SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_rows, dim3((unsigned)((x.fblocks + z.fblocks) * blocks), (unsigned)((R + 15) / 16), (unsigned)g.adapters), dim3(512), s, g, x, z,
+                block_sum(gx), block_sum(gz), R, blocks > 1 ? 0 : accumulate, ids, counts);
+    const int ablocks = (a.C + 1023) / 1024, bblocks = (b.C + 1023) / 1024;
+    if (blocks > 1)
+      SSTE_LAUNCH(SSTE_K_ADAPTER, k_adapter_outer_rows_sum, dim3((unsigned)(ablocks + bblocks), (unsigned)R, (unsigned)g.adapters), dim3(256), s, R, blocks, gx, gz, ablocks, counts, accumulate);
     return hipGetLastError();
   }
   const OuterArgs x = args(a, (float*)ws), z = args(b, (float*)ws + slots(g, chunk) * R * a.C);

@@ -121,6 +121,26 @@ size_t sste_adapter_wgrad_workspace_bytes(int64_t T, int64_t segments, int64_t R
   return adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
 }
 
+// What a call needs whose number of adapters is known; never more than the same without that number
+static size_t wgrad_workspace(int64_t T, int64_t segments, int64_t adapters, int64_t R, int64_t I, int64_t O) {
+  switch (wgrad_way(T, segments, adapters, (int)R, I, O)) {
+    case kWgradFew: return segments <= adapters ? adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O) : 0;
+    case kWgradRows: return wgrad_rows_workspace_bytes(T, adapters, (int)R, I, O);
+    default: return adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);
+  }
+}
+
+size_t sste_adapter_wgrad_workspace_bytes_ex(int64_t T, int64_t segments, int64_t adapters, int64_t R, int64_t I, int64_t O) {
+  const char* who = "adapter_wgrad_workspace_bytes_ex";
+  clear_error();
+  if (check_sizes(who, T, segments, R, I, O) != SSTE_OK) return 0;
+  if (adapters < 0 || adapters > kAdapterMaxAdapters) {
+    fail(SSTE_ERR_SHAPE, "%s: %lld adapters", who, (long long)adapters);
+    return 0;
+  }
+  return wgrad_workspace(T, segments, adapters, R, I, O);
+}
+
 int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int dtype, float dz_scale,
                        const void* X, int64_t I, int64_t ldx, int x_dtype, float x_scale, const void* x_blocks, int64_t ldxb,
                        const float* S, int64_t lds, const float* dS, int64_t ldds,
@@ -151,8 +171,8 @@ int sste_adapter_wgrad(const void* dZ, int64_t T, int64_t O, int64_t lddz, int d
   TRY(check_matrix(who, "dS", dS, T, R, ldds, 4));
   TRY(check_matrix(who, "dA", dA, adapters * R, I, ldda, 4));
   TRY(check_matrix(who, "dB", dB, adapters * R, O, lddb, 4));
-  const size_t need = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O);      // R x (I + O) floats for each chunk
-  if (need > 0 && product_reaches((int64_t)(need / (4 * (size_t)R * (size_t)(I + O))), 2 * (I / 256 + O / 256 + 2), kAdapterMaxGrid))
+  const size_t chunks = adapter_wgrad_workspace_bytes(T, (int)segments, (int)R, I, O), need = wgrad_workspace(T, segments, adapters, R, I, O);
+  if (chunks > 0 && product_reaches((int64_t)(chunks / (4 * (size_t)R * (size_t)(I + O))), 2 * (I / 256 + O / 256 + 2), kAdapterMaxGrid))      // R x (I + O) floats for each
     return fail(SSTE_ERR_UNSUPPORTED, "%s: more than 2^24 tiles", who);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(SSTE_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace ? workspace_bytes : (size_t)0, need);

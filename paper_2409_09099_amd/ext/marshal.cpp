@@ -47,7 +47,7 @@ decltype(&sste_adapter_fwd) p_adapter_fwd;
 decltype(&sste_adapter_dgrad) p_adapter_dgrad;
 decltype(&sste_adapter_wgrad) p_adapter_wgrad;
 decltype(&sste_adapter_workspace_bytes) p_adapter_workspace_bytes;
-decltype(&sste_adapter_wgrad_workspace_bytes) p_adapter_wgrad_workspace_bytes;
+decltype(&sste_adapter_wgrad_workspace_bytes_ex) p_adapter_wgrad_workspace_bytes;
 decltype(&sste_checkpoint_pack) p_checkpoint_pack;
 decltype(&sste_checkpoint_backward) p_checkpoint_backward;
 decltype(&sste_last_error) p_last_error;
@@ -504,7 +504,7 @@ PyObject* adapter_wgrad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyOb
   if (!a.ok || dA->scalar_type() != at::kFloat || dB->scalar_type() != at::kFloat || ga.n != n || gb.n != n || ga.rank != R || gb.rank != R || ga.width != x.cols || gb.width != y.cols)
     return decline(ADAPTER_WGRAD, args, nargs, kwnames);
   if (!ws) {
-    scratch = at::empty({(int64_t)p_adapter_wgrad_workspace_bytes(x.rows, n_seg, R, x.cols, y.cols)}, at::TensorOptions().dtype(at::kByte).device(X->device()));
+    scratch = at::empty({(int64_t)p_adapter_wgrad_workspace_bytes(x.rows, n_seg, n, R, x.cols, y.cols)}, at::TensorOptions().dtype(at::kByte).device(X->device()));
     ws = &scratch;
   }
   const size_t ws_bytes = (size_t)ws->numel() * ws->element_size();
@@ -631,7 +631,7 @@ PyObject* bind(PyObject*, PyObject* args) {
           take(addr, "sste_wgrad_workspace_bytes", p_wgrad_workspace_bytes) && take(addr, "sste_cast_fp8", p_cast_fp8) &&
           take(addr, "sste_project_pack_batch", p_project_pack_batch) && take(addr, "sste_sgd_project_pack_batch", p_sgd_project_pack_batch) &&
           take(addr, "sste_adapter_fwd", p_adapter_fwd) && take(addr, "sste_adapter_dgrad", p_adapter_dgrad) && take(addr, "sste_adapter_wgrad", p_adapter_wgrad) &&
-          take(addr, "sste_adapter_workspace_bytes", p_adapter_workspace_bytes) && take(addr, "sste_adapter_wgrad_workspace_bytes", p_adapter_wgrad_workspace_bytes) && take(addr, "sste_checkpoint_pack", p_checkpoint_pack) &&
+          take(addr, "sste_adapter_workspace_bytes", p_adapter_workspace_bytes) && take(addr, "sste_adapter_wgrad_workspace_bytes_ex", p_adapter_wgrad_workspace_bytes) && take(addr, "sste_checkpoint_pack", p_checkpoint_pack) &&
           take(addr, "sste_checkpoint_backward", p_checkpoint_backward) && take(addr, "sste_last_error", p_last_error)))
       return nullptr;
     g_bound = true;
