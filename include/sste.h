@@ -577,7 +577,8 @@ size_t sste_adapter_wgrad_workspace_bytes_ex(int64_t T, int64_t segments, int64_
  *                             code = RNE_e4m3(x * 2^-e), scale byte = e + 127.  No element saturates; relative to an element the error is at
  *                             most 2^-4, and below 2^-6 * 2^e an absolute 2^-10 * 2^e.  Infinities and NaN become NaN codes (0x7F or 0xFF) and
  *                             leave the rest of their block alone.
- *   sste_checkpoint_backward  h = code * 2^e (exact in bf16; a magnitude that pack rounded up to 2^128 comes back as an infinity);
+ *   sste_checkpoint_backward  h = code * 2^e (exact in bf16; a magnitude that pack rounded up to 2^128 comes back as an infinity,
+ *                             with the activation and the slope of one: itself or 0, and 1 or 0);
  *                             A = RNE_bf16(act(h)) if A is given: the checkpointed tensor itself (SSTE_ACT_NONE) or the activation that the
  *                             next layer's weight gradient reads; dH = RNE_bf16(dA * act'(h)) if dA and dH are given (with SSTE_ACT_NONE: dA).
  *                             act as in sste_linear_fwd_act.  dH may be dA itself, with the same leading dimension.

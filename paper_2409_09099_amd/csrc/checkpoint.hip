@@ -49,6 +49,10 @@ __device__ __forceinline__ uint32_t top_of(uint32_t w) {
 // x * s as a float for the conversion; an infinity becomes NaN, which e4m3 has and an infinity not
 __device__ __forceinline__ float scaled(uint32_t bits, float s) { return (bits & 0x7FFFFFFF) < 0x7F800000u ? u2f(bits) * s : u2f(0x7FC00000u); }
 
+// For GELU, whose products of zeros and infinities would be NaN: what pack rounded up to 2^128 is the largest float again, whose activation is itself (an infinity
+// as bf16) or zero and whose slope 1 or 0.  NaN stays.
+__device__ __forceinline__ float finite(float h) { return __builtin_fabsf(h) == __builtin_inff() ? __builtin_copysignf(0x1.fffffep127f, h) : h; }
+
 template <int U>
 __global__ void __launch_bounds__(256)
 k_checkpoint_pack(Rows g, const uint8_t* __restrict__ X, int64_t ldx, uint8_t* __restrict__ codes, int64_t ldc, uint8_t* __restrict__ scales, int64_t lds) {
@@ -114,7 +118,8 @@ k_checkpoint_backward(Rows g, const uint8_t* __restrict__ codes, int64_t ldc, co
       uint32_t a[8], h[8];
 #pragma unroll
       for (int k = 0; k < 8; k++) {
-        const f32x2 v = (k & 1) ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k >> 1], s[u], true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k >> 1], s[u], false);
+        f32x2 v = (k & 1) ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k >> 1], s[u], true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[k >> 1], s[u], false);
+        if (GELU) v[0] = finite(v[0]), v[1] = finite(v[1]);
         if (ACT) a[k] = GELU ? bf16_rne_pack(gelu_tanh(v[0]), gelu_tanh(v[1])) : bf16_rne_pack(v[0], v[1]);
         if (GRAD) h[k] = GELU ? bf16_rne_pack(bf16lo_f32(y[k]) * gelu_tanh_grad(v[0]), bf16hi_f32(y[k]) * gelu_tanh_grad(v[1])) : y[k];
       }

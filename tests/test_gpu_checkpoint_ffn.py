@@ -37,3 +37,19 @@ def test_weight_gradient_of_a_restored_activation(T, d, h):
     exact = OL.mvue_dense(dY.view(torch.int16).cpu().numpy().view(np.uint16), 3, 1).T @ a64
     assert (np.abs(dW - exact) <= sums + theta.T @ bound).all()
     assert (np.abs(dW).max(axis=1) > 0).all()
+
+
+def test_the_largest_pre_activations():
+    """Finite ones that e4m3 rounds up to 2^128: the activation goes to infinity or to zero, its slope is 1 or 0, and nothing is NaN."""
+    import paper_2409_09099_amd as sste
+    top = torch.finfo(torch.bfloat16).max
+    H = torch.tensor([[top, -top, 3.3e38, -3.3e38] + [1.0] * 28, [float("nan"), float("inf"), float("-inf"), top] + [0.0] * 28], device="cuda").to(torch.bfloat16)
+    dA = torch.full_like(H, 0.75)
+    codes, scales = sste.checkpoint_pack(H)
+    restored = sste.checkpoint_backward(codes, scales, act=sste.ACT_NONE)[0]
+    assert torch.isinf(restored[0, :4]).all() and restored[1, 3] == float("inf") and restored[1, :3].isnan().all()
+    for A, dH in (sste.checkpoint_backward(codes, scales, dA), (sste.checkpoint_backward(codes, scales)[0], sste.checkpoint_backward(codes, scales, dA, restore=False)[1])):
+        assert A[0, :4].tolist() == [float("inf"), 0.0, float("inf"), 0.0] and A[1, 3] == float("inf")
+        assert dH[0, :4].tolist() == [0.75, 0.0, 0.75, 0.0] and dH[1, 3] == 0.75
+        assert A[1, :3].isnan().all() and dH[1, :3].isnan().all()
+        assert A[0, 4:].isfinite().all() and not A[1, 4:].any() and (dH[1, 4:] == 0.375).all()
