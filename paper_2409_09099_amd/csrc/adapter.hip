@@ -317,7 +317,8 @@ struct Up {
     uint4 old[TT][4];
   };
   static __device__ __forceinline__ void load_ranks(uint32_t (&x)[8][4], int s, BufferRsrc ru, int64_t ldu, uint32_t at) {
-    const int q = ((int)threadIdx.x & 63) >> 4;
+    int q = ((int)threadIdx.x & 63) >> 4;
+    asm("" : "+v"(q));                                  // offsets anew too (rank 64 in one launch, 200 rows of their own: 23.1 us, with spills 28.9)
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const uint32_t r = (RP == 16 ? (q & 1) * 8 : s * 32 + q * 8) + i;
@@ -363,7 +364,9 @@ struct Up {
 #pragma unroll
           for (int j = 0; j < 8; j++) c[j] = (f32x4){0, 0, 0, 0};
         // Of 16 ranks, hi and mid fill one instruction's 32 places, lo half of another's
-        const int row = k * 16 + m, at_rank = RP == 16 ? (q & 1) * 8 : s * 32 + q * 8;
+        int row = k * 16 + m;
+        asm("" : "+v"(row));                              // D from LDS for each 128 features anew: kept over them, it would take registers that the sums need
+        const int at_rank = RP == 16 ? (q & 1) * 8 : s * 32 + q * 8;
         const uint4 hi = *(const uint4*)&parts[RP == 16 ? q >> 1 : 0][row][at_rank], mid = *(const uint4*)&parts[1][row][at_rank];
         uint4 lo = *(const uint4*)&parts[2][row][at_rank];
         if (RP == 16 && q >= 2) lo = make_uint4(0, 0, 0, 0);
