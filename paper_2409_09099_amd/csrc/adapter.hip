@@ -5,7 +5,8 @@
 //   outer  G_n = sum over rows of n of L^T M    R x C, float32       dA (L = dS, M = X), dB (L = S, M = dZ)
 //
 // A and B are both kept rank-major (R x I, R x O), so the forward pass and the input gradient are the same two kernels with A and B
-// exchanged, and the two weight gradients are one.  The rank is small: all three are bound by the bytes of X, base, out and M.
+// exchanged, and the two weight gradients are one.  The rank is small: all three are bound by the bytes of X, base, out and M.  TB/s in these comments count
+// what a kernel has to read and write, once each.
 #include "adapter.h"
 
 #include <cmath>
@@ -408,9 +409,10 @@ __device__ __forceinline__ void bare_features(const Tile& t, int f0, int C, cons
 __device__ __forceinline__ float scale_of(const DownArgs& a, const Tile& t) { return (a.scale ? a.scale[t.adapter] : 1.0f) * a.x_scale; }
 
 // Both products of 16 rows in one launch, for few rows, bound by the launch and four waits for memory in a row (the bounds, the first chunk, the features'
-// ranks, the stores; one row of 1280 -> 3840, rank 16: 5.5 us; 96 rows of 64 adapters, 1280 -> 5120: 8.9 us, 1.7 TB/s): `slices` workgroups share a tile's features, and each computes D for itself.
+// ranks, the stores; one row of 1280 -> 3840, rank 16: 5.5 us; 96 rows of 64 adapters, 1280 -> 5120: 8.6 us, 1.8 TB/s, with a fifth wait for a second round of the search): `slices`
+// workgroups share a tile's features, and each computes D for itself (five times here, 41 KB of the adapter through L2 each).
 template <int DT, int RT>
-__global__ void __launch_bounds__(512, RT <= 4 ? 4 : 2)      // two workgroups a CU up to rank 64 (200 rows of their own, 2560 -> 2560: 23.4 us against 29.4)
+__global__ void __launch_bounds__(512, RT <= 4 ? 4 : 2)      // two workgroups a CU up to rank 64 (200 rows of their own, 2560 -> 2560: 23.1 us against 29.4)
 k_adapter_both(AdapterSegments g, DownArgs d, UpArgs o, Share share) {
   using D = Down<DT, RT, 1>;
   __shared__ __align__(16) uint8_t lds[D::LDS];
@@ -465,9 +467,9 @@ k_adapter_down(AdapterSegments g, DownArgs d, int splits, int span, float* __res
   }
 }
 
-// Up alone, 512 features of a tile's rows in a workgroup of four waves.  Bound by HBM, base read and out written (32768 rows of 5120, rank 32: 117 us, 5.8 TB/s;
-// 16384 rows of 1024, rank 16, with two partial sums: 15.5 us, 4.5 TB/s), with rank 128 by the adapter's way through L2 too (5003 rows of 1280: 13.5 us).  splits > 1: adds the splits' sums in order and scales them; the workgroups of
-// the first features write D.
+// Up alone, 512 features of a tile's rows in a workgroup of four waves.  Bound by HBM, base read and out written (32768 rows of 5120, rank 32: 118 us, 5.7 TB/s;
+// 16384 rows of 1024, rank 16, with two partial sums: 16.8 us, 4.2 TB/s), with rank 128 by the adapter's way through L2 too (5003 rows of 1280: 12.9 us).  splits > 1:
+// adds the splits' sums in order and scales them; the workgroups of the first features write D.
 template <int RP, int TT>
 __global__ void __launch_bounds__(256, RP <= 32 ? 3 : 2)
 k_adapter_up(AdapterSegments g, DownArgs d, UpArgs o, Share share, int splits, const float* __restrict__ part) {
@@ -1000,8 +1002,8 @@ ApplyPlan plan_apply(const AdapterSegments& g, int R, int K, int C, bool workspa
   // from memory, the adapter from L2), by rounds of a workgroup on every CU, the last as if half full, a workgroup as if 256 elements longer than it is; and,
   // with partial sums, of their writes and of each block of features reading them.  The factors are fitted to 446 problems (ranks 8 to 128, bf16 and e4m3,
   // 1280 ... 5120 wide, 700 ... 32768 rows): the choice costs 1.1 % over the best of the eight ways in the mean, 14 % at most, where limits on rows, ranks and
-  // widths cost 4 % and 25 %.  Rank 128, 5003 ragged rows, 1280 -> 3840: 38.1 us in one part, 42.2 in two, 47.9 in four; 3840 -> 1280: 35.0, 33.8, 32.5, and
-  // 28.9 in two of 64-row tiles.
+  // widths cost 4 % and 25 %.  Rank 128, 5003 ragged rows, 1280 -> 3840: 46.4 us in one part, 46.8 in two, 47.3 in four; 3840 -> 1280: 35.5, 33.3, 30.7, and
+  // 28.5 in two of 64-row tiles.
   double best = 0;
   for (int rows = 32; rows <= (rank > 16 ? 64 : 32); rows += 32) {
     chunk = down_chunk(rank, rows), chunks = K > 0 ? (K + chunk - 1) / chunk : 1;
